@@ -12,10 +12,12 @@ import sys
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
-SOURCES = [os.path.join(CSRC, "zero_shard.hip"), os.path.join(CSRC, "zero_lamb.hip")]
+SOURCES = [os.path.join(CSRC, f) for f in ("zero_shard.hip", "zero_lamb.hip", "zero_operators.hip")]
 DEPS = SOURCES + [os.path.join(CSRC, f) for f in ("shard_kernels.hpp", "small_kernels.hpp", "lamb_kernels.hpp",
-                                                  "lamb_small.hpp", "probe_kernels.hpp", "host_common.hpp")] + \
-    [os.path.join(ROOT, "include", "zero_shard.h")]
+                                                  "lamb_small.hpp", "probe_kernels.hpp", "host_common.hpp",
+                                                  "row_ops.hpp", "norm_kernels.hpp", "route_kernels.hpp",
+                                                  "distill_kernels.hpp")] + \
+    [os.path.join(ROOT, "include", f) for f in ("zero_shard.h", "zero_operators.h")]
 LIB = os.path.join(PKG, "libzeroshard.so")
 # The same sources with waits that end at once (shard_kernels.hpp), for the tests of what follows then.
 IMPATIENT_LIB = os.path.join(PKG, "libzeroshard_impatient.so")

@@ -112,6 +112,9 @@ struct Ctx {
     const DevInfo* info = nullptr;
 };
 
+// The device of the calling thread, and a check that `stream` belongs to it.
+int current_device(hipStream_t stream, int* dev);
+
 // A context of (current device, stream), locked for the duration of a call.
 struct CtxLock {
     std::shared_ptr<Ctx> ref;
