@@ -33,12 +33,11 @@ constexpr int kMarkBits = 65536;  // tokens modulo this are marked to find those
 
 template <int NT>
 struct DistillLds {
-    float wave_max[NT / 64], wave_sum[NT / 64], wave_sum1[NT / 64];
-    float wave_top[NT / 64], wave_teacher[NT / 64], wave_loss[NT / 64];
+    float wave_max[NT / 64], wave_sum[NT / 64], wave_sum1[NT / 64], wave_top[NT / 64];
     int32_t wave_any[NT / 64];
     int32_t twice, label_listed;
-    int32_t token[ZERO_DISTILL_MAX_K];
-    float z[ZERO_DISTILL_MAX_K], p[ZERO_DISTILL_MAX_K];
+    int32_t token[ZERO_DISTILL_MAX_K];                       // -1: absent
+    float z[ZERO_DISTILL_MAX_K], teacher[ZERO_DISTILL_MAX_K];  // the entries' logits, both sides'
     uint32_t marks[kMarkBits / 32];
 };
 
@@ -48,54 +47,105 @@ __device__ __forceinline__ float any_f32(const void* p, int64_t i, int dtype) {
                                : BF16::to_f32(static_cast<const uint16_t*>(p)[i]);
 }
 
-// A running maximum and the sums against it.
-struct Running {
-    float m, s, s1;
+// The exponents x = c (f - m) of terms 2^x summed against a maximum m.  binary16 values take one
+// fused operation, c f - cm with cm = c m rounded once: its error is the same in every term and in
+// their sum, so their quotients do not have it.  In the other types c times the lowest value
+// leaves fp32's range, so there the difference comes first.  A row or wave of nothing but -inf
+// is summed against 0.
+template <typename T>
+struct Against {
+    static constexpr bool kFused = T::kLowest == F16::kLowest;
+    float c, m, cm;
+    __device__ __forceinline__ Against(float c_, float m_)
+        : c(c_), m(m_ == -__builtin_inff() ? 0.f : m_), cm(c * m) {}
+    __device__ __forceinline__ float operator()(float f) const {
+        return kFused ? __builtin_fmaf(f, c, -cm) : (f - m) * c;
+    }
+    // A sum against `from`, taken against this, which is not less.  A sum of 0 is that of nothing but
+    // -inf, which has no maximum to go by.
+    __device__ __forceinline__ float moved(float sum, const Against& from) const {
+        return sum == 0.f ? 0.f : sum * exp2_fast(kFused ? from.cm - cm : (from.m - m) * c);
+    }
 };
 
-// The reference that values up to `m` are summed against: finite where m is -inf.
-__device__ __forceinline__ float ref(float m) { return m == -__builtin_inff() ? 0.f : m; }
+// How the soft and the hard term share the exponentials of an element.
+enum DistillKind {
+    kOneSum,   // one temperature: tau = 1, or one of the terms alone
+    kSquare,   // tau = 2: 2^x of temperature 1 is the square of that of temperature 2
+    kTwoSums,  // an exponential for each
+};
 
-// What turns a sum against `from` into one against m >= from (a sum of nothing stays 0).
-__device__ __forceinline__ float rescale(float from, float m, float c) {
-    return m == -__builtin_inff() ? 0.f : exp2_fast((from - m) * c);
+// Keeps the packed row in its registers between two passes over it: without it the compiler holds
+// the first pass's fp32 values for the second, at twice the registers or more.
+__device__ __forceinline__ void keep_packed(u32x4& v) { asm volatile("" : "+v"(v)); }
+
+// This thread's maximum of PER packed values.
+template <typename T>
+__device__ __forceinline__ float max_of(u32x4 v, float m) {
+    if constexpr (T::kLowest == F16::kLowest) {
+        typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+        const f16x8 h = __builtin_bit_cast(f16x8, v);
+        const auto a = __builtin_elementwise_max(h.lo, h.hi);
+        const auto b = __builtin_elementwise_max(a.lo, a.hi);
+        return fmaxf(fmaxf(m, (float)b.x), (float)b.y);
+    } else {
+        float f[T::kPer];
+        T::unpack(v, f);
+#pragma unroll
+        for (int j = 0; j < T::kPer; ++j)
+            m = fmaxf(m, f[j]);
+        return m;
+    }
 }
 
-// The exponent c (f - m) - bits.  The difference comes first: c m would lose digits to a large
-// maximum, and leaves fp32's range for the lowest value of bf16 and f32.
-struct Exponent {
-    float c, m, bits;
-    __device__ __forceinline__ float operator()(float f) const { return __builtin_fmaf(f - m, c, -bits); }
-};
+template <typename T, int KIND>
+__device__ __forceinline__ void add_terms(u32x4 v, const Against<T>& x, const Against<T>& x1, float& s, float& s1) {
+    float f[T::kPer];
+    T::unpack(v, f);
+#pragma unroll
+    for (int j = 0; j < T::kPer; ++j) {
+        const float e = exp2_fast(x(f[j]));
+        s += e;
+        if constexpr (KIND == kSquare)
+            s1 = __builtin_fmaf(e, e, s1);
+        if constexpr (KIND == kTwoSums)
+            s1 += exp2_fast(x1(f[j]));
+    }
+}
 
-template <typename T, int NT, int NV, int MODE>
-__global__ __launch_bounds__(NT) void k_distill(const zero_distill_args_t a, const DistillScalars k,
-                                               int64_t first) {
+// The gradient without the teacher's own terms: a 2^x + a1 2^x1.
+template <typename T, int KIND>
+__device__ __forceinline__ float share(float f, const Against<T>& x, const Against<T>& x1, float a, float a1) {
+    const float e = exp2_fast(x(f));
+    if constexpr (KIND == kSquare)
+        return e * __builtin_fmaf(a1, e, a);
+    if constexpr (KIND == kTwoSums)
+        return __builtin_fmaf(a1, exp2_fast(x1(f)), a * e);
+    return a * e;
+}
+
+template <typename T, int KIND>
+__device__ __forceinline__ u32x4 share_of(u32x4 v, const Against<T>& x, const Against<T>& x1, float a, float a1) {
+    float f[T::kPer];
+    T::unpack(v, f);
+#pragma unroll
+    for (int j = 0; j < T::kPer; ++j)
+        f[j] = share<T, KIND>(f[j], x, x1, a, a1);
+    return T::pack(f);
+}
+
+// NV > 0: the row lies in the registers, NV vectors a thread; NV = 0: it is read as it is needed.
+template <typename T, int NT, int NV, int MODE, int KIND>
+__device__ __forceinline__ void distill_row(const zero_distill_args_t& a, const DistillScalars& k, DistillLds<NT>& lds,
+                                            int64_t row, float weight, int label) {
     using elem = typename T::elem;
     constexpr int kPer = T::kPer, kWaves = NT / 64;
     constexpr bool kInRegisters = NV > 0;
-    __shared__ DistillLds<NT> lds;
     const int t = threadIdx.x, wave = t / 64, lane = t & 63, vocab = (int)a.vocab, entries = a.k;
-    const int64_t row = first + blockIdx.x;
     const float inf = __builtin_inff();
     const elem* z = static_cast<const elem*>(a.logits) + row * a.ld_logits;
     elem* dz = static_cast<elem*>(a.dlogits) + row * a.ld_dlogits;
-    const float weight = a.row_weight ? a.row_weight[row] : 1.f;
-    const int label = a.labels ? a.labels[row] : -1;
-
-    if (weight == 0.f) {  // the row is not looked at
-        if (MODE != kDistillBack && t == 0) {
-            a.loss[row] = 0.f;
-            if (MODE == kDistillLoss && a.stats)
-                a.stats[3 * row] = a.stats[3 * row + 1] = a.stats[3 * row + 2] = 0.f;
-        }
-        if (MODE != kDistillLoss)
-            for (int c = t * kPer; c < vocab; c += NT * kPer)
-                store_row<T>(dz, c, vocab, u32x4{0, 0, 0, 0});
-        return;
-    }
-    const bool has_label = k.hard != 0.f && label >= 0 && label < vocab;
-    const bool two = has_label && k.c != k.c1;  // the hard term has a sum of its own
+    const bool has_label = label >= 0;
 
     // the row, on its way while the teacher's list is read
     u32x4 v[kInRegisters ? NV : 1];
@@ -117,7 +167,7 @@ __global__ __launch_bounds__(NT) void k_distill(const zero_distill_args_t a, con
         const float x = any_f32(a.teacher_logits, row * entries + j, a.teacher_dtype);
         const bool present = token >= 0 && token < vocab && x != -inf;
         lds.token[j] = present ? token : -1;
-        lds.p[j] = x;
+        lds.teacher[j] = x;
         lds.z[j] = present ? T::to_f32(z[token]) : 0.f;
         any |= present;
         if (present)
@@ -132,158 +182,102 @@ __global__ __launch_bounds__(NT) void k_distill(const zero_distill_args_t a, con
     }
 
     // the row's maximum and sums, of this thread, then of its wave
-    Running r{-inf, 0.f, 0.f};
+    float m = -inf, s = 0.f, s1 = 0.f;
     if constexpr (MODE == kDistillBack) {
     } else if constexpr (kInRegisters) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            float f[kPer];
-            T::unpack(v[i], f);
-#pragma unroll
-            for (int j = 0; j < kPer; ++j)
-                r.m = fmaxf(r.m, f[j]);
-        }
-        r.m = seg_reduce<64>(r.m, Max());
-        const Exponent x{k.c, ref(r.m), 0.f}, x1{k.c1, ref(r.m), 0.f};
+        for (int i = 0; i < NV; ++i)
+            m = max_of<T>(v[i], m);
+        m = seg_reduce<64>(m, Max());
+        const Against<T> x(k.c, m), x1(k.c1, m);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            float f[kPer];
-            T::unpack(v[i], f);
-#pragma unroll
-            for (int j = 0; j < kPer; ++j)
-                r.s += exp2_fast(x(f[j]));
-            if (two) {
-#pragma unroll
-                for (int j = 0; j < kPer; ++j)
-                    r.s1 += exp2_fast(x1(f[j]));
-            }
+            keep_packed(v[i]);
+            add_terms<T, KIND>(v[i], x, x1, s, s1);
         }
     } else {
         for (int c = t * kPer; c < vocab; c += NT * kPer) {
-            float f[kPer];
-            T::unpack(load_row<T>(z, c, vocab, T::kLowest), f);
-            float m = r.m;
-#pragma unroll
-            for (int j = 0; j < kPer; ++j)
-                m = fmaxf(m, f[j]);
-            if (m > r.m) {
-                r.s *= rescale(r.m, m, k.c);
-                r.s1 *= rescale(r.m, m, k.c1);
-                r.m = m;
+            const u32x4 u = load_row<T>(z, c, vocab, T::kLowest);
+            const float up = max_of<T>(u, m);
+            const Against<T> x(k.c, up), x1(k.c1, up);
+            if (up > m) {
+                s = x.moved(s, Against<T>(k.c, m));
+                s1 = x1.moved(s1, Against<T>(k.c1, m));
+                m = up;
             }
-            const Exponent x{k.c, ref(r.m), 0.f}, x1{k.c1, ref(r.m), 0.f};
-#pragma unroll
-            for (int j = 0; j < kPer; ++j)
-                r.s += exp2_fast(x(f[j]));
-            if (two) {
-#pragma unroll
-                for (int j = 0; j < kPer; ++j)
-                    r.s1 += exp2_fast(x1(f[j]));
-            }
+            add_terms<T, KIND>(u, x, x1, s, s1);
         }
-        const float m = seg_reduce<64>(r.m, Max());
-        r.s *= rescale(r.m, m, k.c);
-        r.s1 *= rescale(r.m, m, k.c1);
-        r.m = m;
+        const float up = seg_reduce<64>(m, Max());
+        s = Against<T>(k.c, up).moved(s, Against<T>(k.c, m));
+        s1 = Against<T>(k.c1, up).moved(s1, Against<T>(k.c1, m));
+        m = up;
     }
-    r.s = seg_reduce<64>(r.s, Add());
-    r.s1 = seg_reduce<64>(r.s1, Add());
+    if constexpr (MODE != kDistillBack) {
+        s = seg_reduce<64>(s, Add());
+        s1 = KIND == kOneSum ? 0.f : seg_reduce<64>(s1, Add());
+    }
     top = seg_reduce<64>(top, Max());
+    any = __ballot(any) != 0;
     if (lane == 0) {
-        lds.wave_max[wave] = r.m;
-        lds.wave_sum[wave] = r.s;
-        lds.wave_sum1[wave] = r.s1;
+        lds.wave_max[wave] = m;
+        lds.wave_sum[wave] = s;
+        lds.wave_sum1[wave] = s1;
         lds.wave_top[wave] = top;
+        lds.wave_any[wave] = any;
     }
-    const bool wave_any = __ballot(any) != 0;
-    if (lane == 0)
-        lds.wave_any[wave] = wave_any;
     __syncthreads();
 
-    top = lds.wave_top[0];
-    any = lds.wave_any[0];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) {
-        top = fmaxf(top, lds.wave_top[w]);
-        any |= lds.wave_any[w] != 0;
-    }
-    const bool has_soft = k.soft_grad != 0.f && any;
-    float m, bits, bits1;  // the maximum, log2 of the sums
+    // of the row: every wave for itself, a lane a wave
+    const int w = lane % kWaves;
+    top = seg_reduce<kWaves>(lds.wave_top[w], Max());
+    const bool has_soft = k.soft_grad != 0.f && __ballot(lds.wave_any[w] != 0) != 0;
     if constexpr (MODE == kDistillBack) {
         m = a.stats[3 * row];
-        bits = a.stats[3 * row + 1];
-        bits1 = a.stats[3 * row + 2];
+        s = a.stats[3 * row + 1];
+        s1 = a.stats[3 * row + 2];
     } else {
-        m = lds.wave_max[0];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w)
-            m = fmaxf(m, lds.wave_max[w]);
-        float s = 0.f, s1 = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            s += lds.wave_sum[w] * rescale(lds.wave_max[w], m, k.c);
-            s1 += lds.wave_sum1[w] * rescale(lds.wave_max[w], m, k.c1);
-        }
-        bits = log2_fast(s);
-        bits1 = two ? log2_fast(s1) : bits;
+        m = seg_reduce<kWaves>(lds.wave_max[w], Max());
+    }
+    const Against<T> x(k.c, m), x1(k.c1, m);
+    if constexpr (MODE != kDistillBack) {
+        const float wm = lds.wave_max[w];
+        s = seg_reduce<kWaves>(x.moved(lds.wave_sum[w], Against<T>(k.c, wm)), Add());
+        s1 = KIND == kOneSum ? s : seg_reduce<kWaves>(x1.moved(lds.wave_sum1[w], Against<T>(k.c1, wm)), Add());
         if (MODE == kDistillLoss && a.stats && t == 0) {
             a.stats[3 * row] = m;
-            a.stats[3 * row + 1] = bits;
-            a.stats[3 * row + 2] = bits1;
+            a.stats[3 * row + 1] = s;
+            a.stats[3 * row + 2] = s1;
         }
     }
-    // log2 of q_tau and q_1
-    const Exponent lq{k.c, m, bits}, lq1{k.c1, m, bits1};
 
-    // the teacher's softmax, and what each entry adds to the loss, in bits
+    // the teacher's softmax, by every wave for itself
+    auto entry = [&](int j) { return (lds.teacher[j] - top) * k.c; };
     float sum = 0.f;
-    for (int j = t; j < entries; j += NT) {
-        const int token = lds.token[j];
-        const float e = token >= 0 && has_soft ? exp2_fast((lds.p[j] - top) * k.c) : 0.f;
-        sum += e;
-    }
+    if (has_soft)
+        for (int j = lane; j < entries; j += 64)
+            sum += lds.token[j] >= 0 ? exp2_fast(entry(j)) : 0.f;
     sum = seg_reduce<64>(sum, Add());
-    if (lane == 0)
-        lds.wave_teacher[wave] = sum;
-    __syncthreads();
-    sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w)
-        sum += lds.wave_teacher[w];
-    const float over = has_soft ? 1.f / sum : 0.f, bits_teacher = has_soft ? log2_fast(sum) : 0.f;
-    float loss = 0.f;
-    for (int j = t; j < entries; j += NT) {
-        const int token = lds.token[j];
-        if (token < 0)
-            continue;
-        const float x = (lds.p[j] - top) * k.c;
-        const float p = has_soft ? exp2_fast(x) * over : 0.f;
-        if (p != 0.f)
-            loss += p * ((x - bits_teacher) - lq(lds.z[j]));
-        lds.p[j] = p;
-        if (MODE != kDistillLoss && has_soft) {
-            const uint32_t bit = 1u << (token & 31);
-            if (atomicOr(&lds.marks[token % kMarkBits / 32], bit) & bit)
-                lds.twice = 1;
-            if (token == label && has_label)
-                lds.label_listed = 1;
-        }
-    }
+    const float over = has_soft ? 1.f / sum : 0.f;
+
     if constexpr (MODE != kDistillBack) {
-        loss = seg_reduce<64>(loss, Add());
-        if (lane == 0)
-            lds.wave_loss[wave] = loss;
-    }
-    __syncthreads();
-    if constexpr (MODE != kDistillBack) {
-        if (t == 0) {
-            float l = 0.f;
-            for (int w = 0; w < kWaves; ++w)
-                l += lds.wave_loss[w];
-            l = has_soft ? l * k.soft_loss : 0.f;
-            if (has_label)
-                l += k.hard * 0.6931471805599453f * -lq1(z_label);
-            a.loss[row] = weight * l;
+        if (wave == 0) {
+            float loss = 0.f;
+            if (has_soft) {
+                const float bits = log2_fast(s) - log2_fast(sum);
+                for (int j = lane; j < entries; j += 64) {
+                    const float p = lds.token[j] >= 0 ? exp2_fast(entry(j)) * over : 0.f;
+                    if (p != 0.f)  // log2 p - log2 q
+                        loss += p * ((entry(j) - x(lds.z[j])) + bits);
+                }
+                loss = seg_reduce<64>(loss, Add()) * k.soft_loss;
+            }
+            if (has_label) {
+                // at temperature 1 kSquare has twice the exponent of temperature 2
+                const float xl = KIND == kSquare ? 2.f * x(z_label) : KIND == kTwoSums ? x1(z_label) : x(z_label);
+                loss += k.hard * 0.6931471805599453f * (log2_fast(s1) - xl);
+            }
+            if (lane == 0)
+                a.loss[row] = weight * loss;
         }
     }
 
@@ -291,38 +285,39 @@ __global__ __launch_bounds__(NT) void k_distill(const zero_distill_args_t a, con
         float up = weight * k.scale;
         if (MODE == kDistillBack && a.dloss)
             up *= a.dloss[row];
-        // gradient = soft_up q_tau + hard_up q_1 - (the teacher's and the label's own)
         const float soft_up = has_soft ? up * k.soft_grad : 0.f, hard_up = has_label ? up * k.hard : 0.f;
-        auto share = [&](float f) {
-            float g = 0.f;
-            if (has_soft)
-                g = soft_up * exp2_fast(lq(f));
-            if (has_label)
-                g = __builtin_fmaf(hard_up, exp2_fast(lq1(f)), g);
-            return g;
-        };
+        float f = has_soft ? soft_up / s : 0.f, f1 = has_label ? hard_up / s1 : 0.f;
+        if constexpr (KIND == kOneSum) {
+            f += f1;
+            f1 = 0.f;
+        }
+        if (!has_soft && !has_label) {  // no term: nothing of the row counts
+            for (int c = t * kPer; c < vocab; c += NT * kPer)
+                store_row<T>(dz, c, vocab, u32x4{0, 0, 0, 0});
+            return;
+        }
+        for (int j = t; j < entries && has_soft; j += NT) {
+            const int token = lds.token[j];
+            if (token >= 0) {
+                const uint32_t bit = 1u << (token & 31);
+                if (atomicOr(&lds.marks[token % kMarkBits / 32], bit) & bit)
+                    lds.twice = 1;
+                if (token == label)
+                    lds.label_listed = 1;
+            }
+        }
         if constexpr (kInRegisters) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int c = (t + i * NT) * kPer;
-                if (c < vocab) {
-                    float f[kPer];
-                    T::unpack(v[i], f);
-#pragma unroll
-                    for (int j = 0; j < kPer; ++j)
-                        f[j] = share(f[j]);
-                    store_row<T>(dz, c, vocab, T::pack(f));
-                }
+                keep_packed(v[i]);
+                if (c < vocab)
+                    store_row<T>(dz, c, vocab, share_of<T, KIND>(v[i], x, x1, f, f1));
             }
         } else {
-            for (int c = t * kPer; c < vocab; c += NT * kPer) {
-                float f[kPer];
-                T::unpack(load_row<T>(z, c, vocab, T::kLowest), f);
-#pragma unroll
-                for (int j = 0; j < kPer; ++j)
-                    f[j] = share(f[j]);
-                store_row<T>(dz, c, vocab, T::pack(f));
-            }
+            for (int c = t * kPer; c < vocab; c += NT * kPer)
+                store_row<T>(dz, c, vocab,
+                             share_of<T, KIND>(load_row<T>(z, c, vocab, T::kLowest), x, x1, f, f1));
         }
         // the tokens with a term of their own, over what was just stored: the barrier orders the
         // workgroup's stores before these
@@ -333,21 +328,50 @@ __global__ __launch_bounds__(NT) void k_distill(const zero_distill_args_t a, con
                 const int token = lds.token[j];
                 if (token < 0)
                     continue;
-                float p = lds.p[j];
+                float p = exp2_fast(entry(j));
                 if (twice) {  // a token listed again: every one of its entries writes the whole sum
                     p = 0.f;
                     for (int i = 0; i < entries; ++i)
-                        p += lds.token[i] == token ? lds.p[i] : 0.f;
+                        p += lds.token[i] == token ? exp2_fast(entry(i)) : 0.f;
                 }
-                float g = share(lds.z[j]) - soft_up * p;
-                if (has_label && token == label)
-                    g -= hard_up;
-                dz[token] = T::of_f32(g);
+                const float own = soft_up * (p * over) + (token == label ? hard_up : 0.f);
+                dz[token] = T::of_f32(share<T, KIND>(lds.z[j], x, x1, f, f1) - own);
             }
         }
         if (t == 0 && has_label && !(has_soft && lds.label_listed))
-            dz[label] = T::of_f32(share(z_label) - hard_up);
+            dz[label] = T::of_f32(share<T, KIND>(z_label, x, x1, f, f1) - hard_up);
     }
+}
+
+template <typename T, int NT, int NV, int MODE>
+__global__ __launch_bounds__(NT) void k_distill(const zero_distill_args_t a, const DistillScalars k,
+                                               int64_t first) {
+    __shared__ DistillLds<NT> lds;
+    const int64_t row = first + blockIdx.x;
+    const float weight = a.row_weight ? a.row_weight[row] : 1.f;
+    int label = a.labels ? a.labels[row] : -1;
+    if (weight == 0.f) {  // the row is not looked at
+        if (MODE != kDistillBack && threadIdx.x == 0) {
+            a.loss[row] = 0.f;
+            if (MODE == kDistillLoss && a.stats)
+                a.stats[3 * row] = a.stats[3 * row + 1] = a.stats[3 * row + 2] = 0.f;
+        }
+        if (MODE != kDistillLoss) {
+            typename T::elem* dz = static_cast<typename T::elem*>(a.dlogits) + row * a.ld_dlogits;
+            for (int c = threadIdx.x * T::kPer; c < (int)a.vocab; c += NT * T::kPer)
+                store_row<T>(dz, c, (int)a.vocab, u32x4{0, 0, 0, 0});
+        }
+        return;
+    }
+    if (k.hard == 0.f || label >= a.vocab)
+        label = -1;
+    // the same for the whole workgroup
+    if (label < 0 || k.c == k.c1)
+        distill_row<T, NT, NV, MODE, kOneSum>(a, k, lds, row, weight, label);
+    else if (2.f * k.c == k.c1)
+        distill_row<T, NT, NV, MODE, kSquare>(a, k, lds, row, weight, label);
+    else
+        distill_row<T, NT, NV, MODE, kTwoSums>(a, k, lds, row, weight, label);
 }
 
 }  // namespace zo

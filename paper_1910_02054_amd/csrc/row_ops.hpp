@@ -203,11 +203,7 @@ __device__ __forceinline__ V row_reduce(V x, V* lds, OP op) {
         if ((threadIdx.x & 63) == 0)
             lds[threadIdx.x / 64] = x;
         __syncthreads();
-        V r = lds[0];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w)
-            r = op(r, lds[w]);
-        return r;
+        return seg_reduce<kWaves>(lds[threadIdx.x % kWaves], op);
     }
 }
 

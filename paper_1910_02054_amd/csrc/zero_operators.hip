@@ -328,7 +328,7 @@ int distill(const char* fn, const zero_distill_args_t* args, void* stream_) {
 
     const double log2e = 1.4426950408889634074, ln2 = 0.69314718055994530942;
     zo::DistillScalars k;
-    k.c = (float)(log2e / a.temperature);
+    k.c = (float)(log2e / (a.soft != 0.0 ? a.temperature : 1.0));  // the hard term alone is of temperature 1
     k.c1 = (float)log2e;
     k.soft_loss = (float)(a.soft * a.temperature * a.temperature * ln2);
     k.soft_grad = (float)(a.soft * a.temperature);
@@ -345,7 +345,7 @@ int distill(const char* fn, const zero_distill_args_t* args, void* stream_) {
             return ZERO_OK;
         };
         const int64_t vectors = div_up(a.vocab, T::kPer);
-        if constexpr (MODE == zo::kDistillStep)
+        if constexpr (MODE != zo::kDistillBack)
             return with_distill_shape(vectors, launch);
         else
             return with_stream_shape(vectors, launch);
