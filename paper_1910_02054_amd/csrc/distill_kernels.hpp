@@ -3,14 +3,17 @@
 //
 // With c = log2(e) / tau and m the row's maximum, q_tau[v] = 2^(c z_v - c m) / S; the
 // gradient is q's multiple but at the teacher's few tokens and the label.  So a row
-// needs its maximum, one or two sums (of temperature tau for the soft term, of 1 for the hard
-// one), and k gathered logits; then one pass writes multiples of q, and the few tokens are
-// written once more with their whole value.
+// needs its maximum and one or two sums (of temperature tau for the soft term, of 1 for the hard
+// one); then one pass writes multiples of q, less what the few tokens have of their own.
 //
 // A workgroup takes a row.  In the step it is read once and kept in registers (NV 16-byte
 // vectors a thread) until its gradient is written, so HBM sees one read and one write; each
 // wave sums against its own maximum, so that maximum and sums cross the workgroup together,
-// behind one barrier.
+// behind one barrier.  The few tokens' logits are gathered while the row is on its way, and their
+// values are written once more, whole, over what the row's pass has stored.  (Putting the vectors that
+// hold a listed token aside in LDS and writing each value once takes longer: a look at a mark for
+// every vector costs more than the few lines that are written twice; 4096 rows of 50304
+// f16 with 64 entries 155 us in place of 144.)
 #pragma once
 
 #include "row_ops.hpp"
@@ -29,17 +32,19 @@ struct DistillScalars {
     float scale;
 };
 
-constexpr int kMarkBits = 65536;  // tokens modulo this are marked to find those listed twice
+constexpr int kMaxEdges = zs::kLineBytes / 2 + 8;  // bound of Cut::edges
 
 template <int NT>
 struct DistillLds {
     float wave_max[NT / 64], wave_sum[NT / 64], wave_sum1[NT / 64], wave_top[NT / 64];
     int32_t wave_any[NT / 64];
-    int32_t twice, label_listed;
-    int32_t token[ZERO_DISTILL_MAX_K];                       // -1: absent
-    float z[ZERO_DISTILL_MAX_K], teacher[ZERO_DISTILL_MAX_K];  // the entries' logits, both sides'
-    uint32_t marks[kMarkBits / 32];
 };
+
+// Dynamic LDS of a row of k entries and the label: tokens, both sides' logits, and where a gradient is
+// written the chains in which an entry finds those of its own token: links, and `heads`, a power of two.
+constexpr int64_t distill_lds_bytes(int k, int heads, int mode) {
+    return 12 * (int64_t)(k + 1) + (mode == kDistillLoss ? 0 : 4 * (int64_t)(k + 1 + heads));
+}
 
 __device__ __forceinline__ float any_f32(const void* p, int64_t i, int dtype) {
     return dtype == ZERO_F32   ? static_cast<const float*>(p)[i]
@@ -47,26 +52,45 @@ __device__ __forceinline__ float any_f32(const void* p, int64_t i, int dtype) {
                                : BF16::to_f32(static_cast<const uint16_t*>(p)[i]);
 }
 
-// The exponents x = c (f - m) of terms 2^x summed against a maximum m.  binary16 values take one
-// fused operation, c f - cm with cm = c m rounded once: its error is the same in every term and in
-// their sum, so their quotients do not have it.  In the other types c times the lowest value
-// leaves fp32's range, so there the difference comes first.  A row or wave of nothing but -inf
-// is summed against 0.
+// The exponents x = c (f - m) of terms 2^x summed against a maximum m.  A row or wave of nothing
+// but -inf is summed against 0.
+//
+// The 16-bit types take one fused operation, c f - cm, where cm = c m is rounded once.  That
+// shifts every x of a row by the same amount (`shift`), which the quotients of terms and their sum
+// do not have; `log` takes it out.  The shift is small while cm is: from 2^20 on (logits
+// no model has, but a row may hold nothing but the type's lowest value) neighbouring values
+// of the type lie at least 2^9 apart in x, so a term is 1 or 0 whatever the scale, and a
+// smaller c keeps cm at 2^20.  fp32 takes the difference first: its bytes leave the time for it.
 template <typename T>
 struct Against {
-    static constexpr bool kFused = T::kLowest == F16::kLowest;
-    float c, m, cm;
+    static constexpr bool kFused = sizeof(typename T::elem) == 2;
+    float c, m, cm, whole;  // whole: c as given
     __device__ __forceinline__ Against(float c_, float m_)
-        : c(c_), m(m_ == -__builtin_inff() ? 0.f : m_), cm(c * m) {}
+        : c(c_), m(m_ == -__builtin_inff() ? 0.f : m_), cm(c * m), whole(c_) {
+        if (kFused && fabsf(cm) >= 0x1p20f && fabsf(m) < __builtin_inff()) {
+            c = 0x1p20f / fabsf(m);
+            cm = c * m;
+        }
+    }
     __device__ __forceinline__ float operator()(float f) const {
         return kFused ? __builtin_fmaf(f, c, -cm) : (f - m) * c;
     }
     // A sum against `from`, taken against this, which is not less.  A sum of 0 is that of nothing but
     // -inf, which has no maximum to go by.
     __device__ __forceinline__ float moved(float sum, const Against& from) const {
-        return sum == 0.f ? 0.f : sum * exp2_fast(kFused ? from.cm - cm : (from.m - m) * c);
+        return sum == 0.f ? 0.f : sum * exp2_fast(kFused && c == from.c ? from.cm - cm : (from.m - m) * c);
+    }
+    // log2 of the quotient of f's term and the sum of all.
+    __device__ __forceinline__ float log(float f, float sum) const {
+        const float shift = kFused ? (*this)(m) : 0.f;
+        return (f - m) * whole - (log2_fast(sum) - shift);
     }
 };
+
+constexpr int kBatch = 4;  // vectors at a time of a row that is read as it is needed
+
+// Whether a row goes past the caches.
+constexpr bool past_caches(int threads) { return threads >= 1024; }
 
 // How the soft and the hard term share the exponentials of an element.
 enum DistillKind {
@@ -99,18 +123,22 @@ __device__ __forceinline__ float max_of(u32x4 v, float m) {
 }
 
 template <typename T, int KIND>
+__device__ __forceinline__ void add_term(float f, const Against<T>& x, const Against<T>& x1, float& s, float& s1) {
+    const float e = exp2_fast(x(f));
+    s += e;
+    if constexpr (KIND == kSquare)
+        s1 = __builtin_fmaf(e, e, s1);
+    if constexpr (KIND == kTwoSums)
+        s1 += exp2_fast(x1(f));
+}
+
+template <typename T, int KIND>
 __device__ __forceinline__ void add_terms(u32x4 v, const Against<T>& x, const Against<T>& x1, float& s, float& s1) {
     float f[T::kPer];
     T::unpack(v, f);
 #pragma unroll
-    for (int j = 0; j < T::kPer; ++j) {
-        const float e = exp2_fast(x(f[j]));
-        s += e;
-        if constexpr (KIND == kSquare)
-            s1 = __builtin_fmaf(e, e, s1);
-        if constexpr (KIND == kTwoSums)
-            s1 += exp2_fast(x1(f[j]));
-    }
+    for (int j = 0; j < T::kPer; ++j)
+        add_term<T, KIND>(f[j], x, x1, s, s1);
 }
 
 // The gradient without the teacher's own terms: a 2^x + a1 2^x1.
@@ -125,87 +153,127 @@ __device__ __forceinline__ float share(float f, const Against<T>& x, const Again
 }
 
 template <typename T, int KIND>
-__device__ __forceinline__ u32x4 share_of(u32x4 v, const Against<T>& x, const Against<T>& x1, float a, float a1) {
-    float f[T::kPer];
-    T::unpack(v, f);
+__device__ __forceinline__ void share_of(u32x4 v, const Against<T>& x, const Against<T>& x1, float a, float a1,
+                                         float* g) {
+    T::unpack(v, g);
 #pragma unroll
     for (int j = 0; j < T::kPer; ++j)
-        f[j] = share<T, KIND>(f[j], x, x1, a, a1);
-    return T::pack(f);
+        g[j] = share<T, KIND>(g[j], x, x1, a, a1);
 }
 
 // NV > 0: the row lies in the registers, NV vectors a thread; NV = 0: it is read as it is needed.
 template <typename T, int NT, int NV, int MODE, int KIND>
 __device__ __forceinline__ void distill_row(const zero_distill_args_t& a, const DistillScalars& k, DistillLds<NT>& lds,
-                                            int64_t row, float weight, int label) {
+                                            int heads, int64_t row, float weight, int label) {
     using elem = typename T::elem;
     constexpr int kPer = T::kPer, kWaves = NT / 64;
     constexpr bool kInRegisters = NV > 0;
+    constexpr bool kPast = past_caches(NT);
+    static_assert(NT >= kMaxEdges, "a thread for each edge element");
     const int t = threadIdx.x, wave = t / 64, lane = t & 63, vocab = (int)a.vocab, entries = a.k;
     const float inf = __builtin_inff();
     const elem* z = static_cast<const elem*>(a.logits) + row * a.ld_logits;
     elem* dz = static_cast<elem*>(a.dlogits) + row * a.ld_dlogits;
     const bool has_label = label >= 0;
+    // entry `entries` is the label
+    const int all = entries + 1;
+    extern __shared__ int32_t room[];
+    int32_t* const token_of = room;  // -1: absent
+    float* const teacher_of = reinterpret_cast<float*>(room + all);
+    float* const z_of = reinterpret_cast<float*>(room + 2 * all);
+    int32_t* const next_of = room + 3 * all;
+    int32_t* const head_of = room + 4 * all;
+    // vectors begin at a line of the row that is written (or read), so that a wave's accesses are whole
+    // lines wherever a row starts (a vocabulary of 50257 has rows at every place of a line)
+    const Cut<T> cut(MODE == kDistillLoss ? z : dz, vocab);
+    const elem* zv = z + cut.head;
 
-    // the row, on its way while the teacher's list is read
+    // the first of the teacher's entries, then the row, so that the list is there before it
+    int token = -1;
+    float x_teacher = 0.f;
+    if (t < entries) {
+        token = a.teacher_index[row * entries + t];
+        x_teacher = any_f32(a.teacher_logits, row * entries + t, a.teacher_dtype);
+    } else if (t == entries) {
+        token = label;
+    }
     u32x4 v[kInRegisters ? NV : 1];
     if constexpr (kInRegisters) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = (t + i * NT) * kPer;
+            const int n = t + i * NT;
             v[i] = u32x4{T::kLowest, T::kLowest, T::kLowest, T::kLowest};
-            if (c < vocab)
-                v[i] = load_row<T>(z, c, vocab, T::kLowest);
+            if (n < cut.vectors)
+                v[i] = load_vec<T, kPast>(zv + n * kPer);
+        }
+    }
+    const bool has_edge = t < cut.edges;
+    const int edge_column = cut.edge_column(t);
+    const float edge = has_edge ? T::to_f32(z[edge_column]) : -inf;
+
+    if constexpr (MODE != kDistillLoss)
+        for (int i = t; i < heads; i += NT)
+            head_of[i] = -1;
+    float top = -inf;  // the teacher's largest logit
+    bool any = false;
+    for (int j = t; j < all; j += NT) {
+        if (j != t) {
+            token = j < entries ? a.teacher_index[row * entries + j] : label;
+            x_teacher = j < entries ? any_f32(a.teacher_logits, row * entries + j, a.teacher_dtype) : 0.f;
+        }
+        const bool present = token >= 0 && token < vocab && x_teacher != -inf;
+        token_of[j] = present ? token : -1;
+        teacher_of[j] = x_teacher;
+        z_of[j] = present ? T::to_f32(z[token]) : 0.f;
+        if (present && j < entries) {
+            any = true;
+            top = fmaxf(top, x_teacher);  // a NaN loses here and counts in the sum
         }
     }
 
-    // the teacher's entries; `top` is their largest logit
-    float top = -inf;
-    bool any = false;
-    for (int j = t; j < entries; j += NT) {
-        const int token = a.teacher_index[row * entries + j];
-        const float x = any_f32(a.teacher_logits, row * entries + j, a.teacher_dtype);
-        const bool present = token >= 0 && token < vocab && x != -inf;
-        lds.token[j] = present ? token : -1;
-        lds.teacher[j] = x;
-        lds.z[j] = present ? T::to_f32(z[token]) : 0.f;
-        any |= present;
-        if (present)
-            top = fmaxf(top, x);  // a NaN loses here and counts in the sum
-    }
-    const float z_label = has_label ? T::to_f32(z[label]) : 0.f;
-    if constexpr (MODE != kDistillLoss) {
-        for (int i = t; i < kMarkBits / 32; i += NT)
-            lds.marks[i] = 0;
-        if (t == 0)
-            lds.twice = lds.label_listed = 0;
-    }
-
     // the row's maximum and sums, of this thread, then of its wave
-    float m = -inf, s = 0.f, s1 = 0.f;
-    if constexpr (MODE == kDistillBack) {
-    } else if constexpr (kInRegisters) {
+    float m = edge, s = 0.f, s1 = 0.f;
+    if constexpr (kInRegisters) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             m = max_of<T>(v[i], m);
         m = seg_reduce<64>(m, Max());
         const Against<T> x(k.c, m), x1(k.c1, m);
+        add_term<T, KIND>(edge, x, x1, s, s1);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             keep_packed(v[i]);
             add_terms<T, KIND>(v[i], x, x1, s, s1);
         }
-    } else {
-        for (int c = t * kPer; c < vocab; c += NT * kPer) {
-            const u32x4 u = load_row<T>(z, c, vocab, T::kLowest);
-            const float up = max_of<T>(u, m);
+    } else if constexpr (MODE != kDistillBack) {
+        {
+            m = edge == edge ? edge : -inf;
+            const Against<T> x(k.c, m), x1(k.c1, m);
+            add_term<T, KIND>(edge, x, x1, s, s1);
+        }
+        for (int n0 = t; n0 < cut.vectors; n0 += kBatch * NT) {
+            u32x4 u[kBatch];
+            float up = m;
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                u[i] = u32x4{T::kLowest, T::kLowest, T::kLowest, T::kLowest};
+                if (n0 + i * NT < cut.vectors)
+                    u[i] = load_vec<T, false>(zv + (n0 + i * NT) * kPer);
+            }
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                up = max_of<T>(u[i], up);
             const Against<T> x(k.c, up), x1(k.c1, up);
             if (up > m) {
                 s = x.moved(s, Against<T>(k.c, m));
                 s1 = x1.moved(s1, Against<T>(k.c1, m));
                 m = up;
             }
-            add_terms<T, KIND>(u, x, x1, s, s1);
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                keep_packed(u[i]);
+                add_terms<T, KIND>(u[i], x, x1, s, s1);
+            }
         }
         const float up = seg_reduce<64>(m, Max());
         s = Against<T>(k.c, up).moved(s, Against<T>(k.c, m));
@@ -250,32 +318,34 @@ __device__ __forceinline__ void distill_row(const zero_distill_args_t& a, const 
         }
     }
 
-    // the teacher's softmax, by every wave for itself
-    auto entry = [&](int j) { return (lds.teacher[j] - top) * k.c; };
+    // the teacher's softmax, by every wave for itself: `sum` is of 2^exponent_of
+    auto exponent_of = [&](int j) { return (teacher_of[j] - top) * k.c; };
     float sum = 0.f;
     if (has_soft)
         for (int j = lane; j < entries; j += 64)
-            sum += lds.token[j] >= 0 ? exp2_fast(entry(j)) : 0.f;
+            sum += token_of[j] >= 0 ? exp2_fast(exponent_of(j)) : 0.f;
     sum = seg_reduce<64>(sum, Add());
     const float over = has_soft ? 1.f / sum : 0.f;
 
     if constexpr (MODE != kDistillBack) {
         if (wave == 0) {
+            const float teacher_bits = log2_fast(sum);
             float loss = 0.f;
-            if (has_soft) {
-                const float bits = log2_fast(s) - log2_fast(sum);
-                for (int j = lane; j < entries; j += 64) {
-                    const float p = lds.token[j] >= 0 ? exp2_fast(entry(j)) * over : 0.f;
-                    if (p != 0.f)  // log2 p - log2 q
-                        loss += p * ((entry(j) - x(lds.z[j])) + bits);
+            for (int j = lane; j < all; j += 64) {
+                if (token_of[j] < 0)
+                    continue;
+                const float f = z_of[j];
+                if (j == entries) {
+                    // temperature 1; kSquare's sum has twice the exponents of temperature 2, its shift too
+                    const float shift = Against<T>::kFused && KIND == kSquare ? 2.f * x(m) - x1(m) : 0.f;
+                    loss -= k.hard * 0.6931471805599453f * (x1.log(f, s1) + shift);
+                } else if (has_soft) {
+                    const float e = exponent_of(j), p = exp2_fast(e) * over;
+                    if (p != 0.f)
+                        loss += k.soft_loss * (p * ((e - teacher_bits) - x.log(f, s)));
                 }
-                loss = seg_reduce<64>(loss, Add()) * k.soft_loss;
             }
-            if (has_label) {
-                // at temperature 1 kSquare has twice the exponent of temperature 2
-                const float xl = KIND == kSquare ? 2.f * x(z_label) : KIND == kTwoSums ? x1(z_label) : x(z_label);
-                loss += k.hard * 0.6931471805599453f * (log2_fast(s1) - xl);
-            }
+            loss = seg_reduce<64>(loss, Add());
             if (lane == 0)
                 a.loss[row] = weight * loss;
         }
@@ -291,61 +361,74 @@ __device__ __forceinline__ void distill_row(const zero_distill_args_t& a, const 
             f += f1;
             f1 = 0.f;
         }
-        if (!has_soft && !has_label) {  // no term: nothing of the row counts
-            for (int c = t * kPer; c < vocab; c += NT * kPer)
-                store_row<T>(dz, c, vocab, u32x4{0, 0, 0, 0});
-            return;
-        }
-        for (int j = t; j < entries && has_soft; j += NT) {
-            const int token = lds.token[j];
-            if (token >= 0) {
-                const uint32_t bit = 1u << (token & 31);
-                if (atomicOr(&lds.marks[token % kMarkBits / 32], bit) & bit)
-                    lds.twice = 1;
-                if (token == label)
-                    lds.label_listed = 1;
-            }
-        }
+        const bool blank = !has_soft && !has_label;  // no term: nothing of the row counts
+        for (int j = t; j < all; j += NT)
+            if (token_of[j] >= 0)
+                next_of[j] = atomicExch(&head_of[token_of[j] & (heads - 1)], j);
+
+        auto write = [&](u32x4 u, int n) __attribute__((always_inline)) {
+            float g[kPer] = {};
+            if (!blank)
+                share_of<T, KIND>(u, x, x1, f, f1, g);
+            store_vec<T, kPast>(dz + cut.head + n * kPer, T::pack(g));
+        };
         if constexpr (kInRegisters) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int c = (t + i * NT) * kPer;
                 keep_packed(v[i]);
-                if (c < vocab)
-                    store_row<T>(dz, c, vocab, share_of<T, KIND>(v[i], x, x1, f, f1));
+                if (t + i * NT < cut.vectors)
+                    write(v[i], t + i * NT);
             }
         } else {
-            for (int c = t * kPer; c < vocab; c += NT * kPer)
-                store_row<T>(dz, c, vocab,
-                             share_of<T, KIND>(load_row<T>(z, c, vocab, T::kLowest), x, x1, f, f1));
-        }
-        // the tokens with a term of their own, over what was just stored: the barrier orders the
-        // workgroup's stores before these
-        __syncthreads();
-        if (has_soft) {
-            const bool twice = lds.twice;
-            for (int j = t; j < entries; j += NT) {
-                const int token = lds.token[j];
-                if (token < 0)
-                    continue;
-                float p = exp2_fast(entry(j));
-                if (twice) {  // a token listed again: every one of its entries writes the whole sum
-                    p = 0.f;
-                    for (int i = 0; i < entries; ++i)
-                        p += lds.token[i] == token ? exp2_fast(entry(i)) : 0.f;
-                }
-                const float own = soft_up * (p * over) + (token == label ? hard_up : 0.f);
-                dz[token] = T::of_f32(share<T, KIND>(lds.z[j], x, x1, f, f1) - own);
+            for (int n0 = t; n0 < cut.vectors; n0 += kBatch * NT) {
+                u32x4 u[kBatch];
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i)
+                    if (n0 + i * NT < cut.vectors)
+                        u[i] = load_vec<T, kPast>(zv + (n0 + i * NT) * kPer);
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i)
+                    if (n0 + i * NT < cut.vectors)
+                        write(u[i], n0 + i * NT);
             }
         }
-        if (t == 0 && has_label && !(has_soft && lds.label_listed))
-            dz[label] = T::of_f32(share<T, KIND>(z_label, x, x1, f, f1) - hard_up);
+        if (has_edge)
+            dz[edge_column] = T::of_f32(blank ? 0.f : share<T, KIND>(edge, x, x1, f, f1));
+
+        // The tokens with a term of their own, over what was just stored: the barrier orders the
+        // workgroup's stores before these.  The first entry of a token writes for all of them.
+        __syncthreads();
+        auto own_of = [&](int j) {
+            return j == entries ? hard_up : has_soft ? soft_up * (exp2_fast(exponent_of(j)) * over) : 0.f;
+        };
+        for (int j = t; j < all && !blank; j += NT) {
+            const int mine = token_of[j];
+            if (mine < 0)
+                continue;
+            int n = 0, first = j, last = j;  // the token's entries
+            for (int i = head_of[mine & (heads - 1)]; i >= 0; i = next_of[i])
+                if (token_of[i] == mine) {
+                    ++n;
+                    first = i < first ? i : first;
+                    last = i > last ? i : last;
+                }
+            if (first != j)
+                continue;
+            float g = share<T, KIND>(z_of[j], x, x1, f, f1) - own_of(j);
+            if (n == 2)
+                g -= own_of(last);
+            else if (n > 2)  // in the entries' order, not the chain's
+                for (int i = j + 1; i < all; ++i)
+                    g -= token_of[i] == mine ? own_of(i) : 0.f;
+            dz[mine] = T::of_f32(g);
+        }
     }
+
 }
 
 template <typename T, int NT, int NV, int MODE>
-__global__ __launch_bounds__(NT) void k_distill(const zero_distill_args_t a, const DistillScalars k,
-                                               int64_t first) {
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT < 1024 || NV <= 7 ? 8 : 4))) void k_distill(
+    const zero_distill_args_t a, const DistillScalars k, int heads, int64_t first) {
     __shared__ DistillLds<NT> lds;
     const int64_t row = first + blockIdx.x;
     const float weight = a.row_weight ? a.row_weight[row] : 1.f;
@@ -358,20 +441,23 @@ __global__ __launch_bounds__(NT) void k_distill(const zero_distill_args_t a, con
         }
         if (MODE != kDistillLoss) {
             typename T::elem* dz = static_cast<typename T::elem*>(a.dlogits) + row * a.ld_dlogits;
-            for (int c = threadIdx.x * T::kPer; c < (int)a.vocab; c += NT * T::kPer)
-                store_row<T>(dz, c, (int)a.vocab, u32x4{0, 0, 0, 0});
+            const Cut<T> cut(dz, (int)a.vocab);
+            for (int n = threadIdx.x; n < cut.vectors; n += NT)
+                store_vec<T, past_caches(NT)>(dz + cut.head + n * T::kPer, u32x4{0, 0, 0, 0});
+            if ((int)threadIdx.x < cut.edges)
+                dz[cut.edge_column(threadIdx.x)] = T::of_f32(0.f);
         }
         return;
     }
-    if (k.hard == 0.f || label >= a.vocab)
+    if (k.hard == 0.f || label >= a.vocab || label < 0)
         label = -1;
     // the same for the whole workgroup
     if (label < 0 || k.c == k.c1)
-        distill_row<T, NT, NV, MODE, kOneSum>(a, k, lds, row, weight, label);
+        distill_row<T, NT, NV, MODE, kOneSum>(a, k, lds, heads, row, weight, label);
     else if (2.f * k.c == k.c1)
-        distill_row<T, NT, NV, MODE, kSquare>(a, k, lds, row, weight, label);
+        distill_row<T, NT, NV, MODE, kSquare>(a, k, lds, heads, row, weight, label);
     else
-        distill_row<T, NT, NV, MODE, kTwoSums>(a, k, lds, row, weight, label);
+        distill_row<T, NT, NV, MODE, kTwoSums>(a, k, lds, heads, row, weight, label);
 }
 
 }  // namespace zo

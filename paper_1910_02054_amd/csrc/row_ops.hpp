@@ -96,12 +96,31 @@ struct BF16 {
     }
 };
 
+// NT: past the caches, for rows that are read or written once and do not come back.
+template <typename T, bool NT>
+__device__ __forceinline__ u32x4 load_vec(const typename T::elem* p) {
+    const typename T::vec* q = reinterpret_cast<const typename T::vec*>(p);
+    if constexpr (NT)
+        return __builtin_nontemporal_load(q);
+    else
+        return *q;
+}
+
+template <typename T, bool NT>
+__device__ __forceinline__ void store_vec(typename T::elem* p, u32x4 v) {
+    typename T::vec* q = reinterpret_cast<typename T::vec*>(p);
+    if constexpr (NT)
+        __builtin_nontemporal_store(v, q);
+    else
+        *q = v;
+}
+
 // The 16 bytes of row `p` from column `col`, elements at or past `cols` filled from
 // `fill` (a word of two or one of them).
 template <typename T>
 __device__ __forceinline__ u32x4 load_row(const typename T::elem* p, int col, int cols, uint32_t fill) {
     if (col + T::kPer <= cols)
-        return *reinterpret_cast<const typename T::vec*>(p + col);
+        return load_vec<T, false>(p + col);
     u32x4 v = {fill, fill, fill, fill};
     if constexpr (T::kPer == 4) {
 #pragma unroll
@@ -123,10 +142,10 @@ __device__ __forceinline__ u32x4 load_row(const typename T::elem* p, int col, in
 }
 
 // Stores the 16 bytes at column `col` of row `p`, but for elements at or past `cols`.
-template <typename T>
+template <typename T, bool NT = false>
 __device__ __forceinline__ void store_row(typename T::elem* p, int col, int cols, u32x4 v) {
     if (col + T::kPer <= cols) {
-        *reinterpret_cast<typename T::vec*>(p + col) = v;
+        store_vec<T, NT>(p + col, v);
         return;
     }
     if constexpr (T::kPer == 4) {
@@ -144,6 +163,24 @@ __device__ __forceinline__ void store_row(typename T::elem* p, int col, int cols
         }
     }
 }
+
+// A row cut at 128-byte lines: its elements before the first line that starts in it, its whole vectors
+// from there, and the elements after them.  Those before and after are its edges, fewer than
+// kLineBytes / sizeof(elem) + kPer: a thread each.
+template <typename T>
+struct Cut {
+    int head, vectors, edges, tail;  // tail: column of the first element after the vectors
+    __device__ __forceinline__ Cut(const typename T::elem* p, int cols) {
+        constexpr int kLine = zs::kLineBytes / (int)sizeof(typename T::elem);
+        const int into = (int)(reinterpret_cast<uintptr_t>(p) / sizeof(typename T::elem)) & (kLine - 1);
+        head = (kLine - into) & (kLine - 1);
+        head = head < cols ? head : cols;
+        vectors = (cols - head) / T::kPer;
+        tail = head + vectors * T::kPer;
+        edges = head + cols - tail;
+    }
+    __device__ __forceinline__ int edge_column(int e) const { return e < head ? e : tail + e - head; }
+};
 
 // ---------------------------------------------------------------------------
 // Reductions.  Steps within rows of 16 lanes by DPP, across them by gfx950's row and

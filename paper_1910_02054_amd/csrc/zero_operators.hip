@@ -336,16 +336,18 @@ int distill(const char* fn, const zero_distill_args_t* args, void* stream_) {
     k.scale = (float)a.grad_scale;
     return with_type(a.dtype, [&](auto type) {
         using T = decltype(type);
+        const int64_t vectors = a.vocab / T::kPer;
+        const int heads = pow2_up(2 * (a.k + 1));
         auto launch = [&](auto shape) {
             using S = decltype(shape);
             for (int64_t first = 0; first < a.rows; first += kMaxLaunch)
                 zo::k_distill<T, S::NT, S::NV, MODE>
-                    <<<(unsigned)std::min(kMaxLaunch, a.rows - first), S::NT, 0, stream>>>(a, k, first);
+                    <<<(unsigned)std::min(kMaxLaunch, a.rows - first), S::NT,
+                       zo::distill_lds_bytes(a.k, heads, MODE), stream>>>(a, k, heads, first);
             HIP_TRY(hipGetLastError());
             return ZERO_OK;
         };
-        const int64_t vectors = div_up(a.vocab, T::kPer);
-        if constexpr (MODE != zo::kDistillBack)
+        if constexpr (MODE == zo::kDistillStep)
             return with_distill_shape(vectors, launch);
         else
             return with_stream_shape(vectors, launch);

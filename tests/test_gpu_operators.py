@@ -499,12 +499,23 @@ def test_distill_terms(zo, dtype):
     check_distill(zo, z, far, teacher, label, weight)
 
 
-def test_distill_tokens_that_share_a_mark(zo):
-    """Distinct tokens 65536 apart take the path of tokens listed twice, and are told apart there."""
+def test_distill_tokens_far_apart(zo):
+    """Tokens a multiple of the tables' sizes apart are told apart."""
     z, index, teacher, label, weight = distill_inputs(2, 140000, 6, F32, F32, 59)
     index[:, :4] = torch.tensor([5, 65541, 131077, 70000], dtype=torch.int32)
     label[:] = torch.tensor([65541, 6], dtype=torch.int32)
     check_distill(zo, z, index, teacher, label, weight)
+
+
+@pytest.mark.parametrize("dtype", C.TYPES)
+@pytest.mark.parametrize("vocab", (300, 5000, 140000))
+def test_distill_crowded(zo, dtype, vocab):
+    """Every token of the first vectors is listed, the label among them."""
+    z, index, teacher, label, weight = distill_inputs(3, vocab, 40, dtype, F32, 60)
+    index[:] = torch.stack([torch.randperm(40, generator=C.rng(5, i)) for i in range(3)]).int()
+    label[:] = torch.tensor([0, 39, 17], dtype=torch.int32)
+    for lead in (0, 5):
+        check_distill(zo, z, index, teacher, label, weight, lead=lead)
 
 
 @pytest.mark.parametrize("dtype", C.TYPES)
