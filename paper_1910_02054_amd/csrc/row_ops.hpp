@@ -200,12 +200,13 @@ __device__ __forceinline__ V swap_step(V x, OP op) {
     return op(__builtin_bit_cast(V, (uint32_t)r[0]), __builtin_bit_cast(V, (uint32_t)r[1]));
 }
 
-// op over segments of L lanes (4, 8, 16, 32 or 64).
+// op over segments of L lanes (2, 4, 8, 16, 32 or 64).
 template <int L, typename V, typename OP>
 __device__ __forceinline__ V seg_reduce(V x, OP op) {
-    static_assert(L == 4 || L == 8 || L == 16 || L == 32 || L == 64, "segment of a wave");
+    static_assert(L == 2 || L == 4 || L == 8 || L == 16 || L == 32 || L == 64, "segment of a wave");
     x = op(x, dpp<0xB1>(x));  // the neighbour
-    x = op(x, dpp<0x4E>(x));  // the other pair
+    if constexpr (L >= 4)
+        x = op(x, dpp<0x4E>(x));  // the other pair
     if constexpr (L >= 8)
         x = op(x, dpp<0x141>(x));  // the other quad (row_half_mirror)
     if constexpr (L >= 16)

@@ -264,8 +264,9 @@ struct DistillShape {
 
 template <typename F>
 int with_distill_shape(int64_t vectors, F f) {
-    if (vectors <= 256) return f(DistillShape<256, 1>{});
-    if (vectors <= 512) return f(DistillShape<256, 2>{});
+    if (vectors <= 128) return f(DistillShape<128, 1>{});
+    if (vectors <= 256) return f(DistillShape<128, 2>{});
+    if (vectors <= 512) return f(DistillShape<128, 4>{});
     if (vectors <= 1024) return f(DistillShape<256, 4>{});
     if (vectors <= 2 * 1024) return f(DistillShape<1024, 2>{});
     if (vectors <= 4 * 1024) return f(DistillShape<1024, 4>{});
@@ -347,7 +348,7 @@ int distill(const char* fn, const zero_distill_args_t* args, void* stream_) {
             HIP_TRY(hipGetLastError());
             return ZERO_OK;
         };
-        if constexpr (MODE == zo::kDistillStep)
+        if constexpr (MODE != zo::kDistillBack)
             return with_distill_shape(vectors, launch);
         else
             return with_stream_shape(vectors, launch);
