@@ -99,10 +99,6 @@ enum DistillKind {
     kTwoSums,  // an exponential for each
 };
 
-// Keeps the packed row in its registers between two passes over it: without it the compiler holds
-// the first pass's fp32 values for the second, at twice the registers or more.
-__device__ __forceinline__ void keep_packed(u32x4& v) { asm volatile("" : "+v"(v)); }
-
 // This thread's maximum of PER packed values.
 template <typename T>
 __device__ __forceinline__ float max_of(u32x4 v, float m) {

@@ -35,24 +35,13 @@ __device__ __forceinline__ uint32_t pack_e4m3(const float* f) {
 }
 
 template <int PER>
-__device__ __forceinline__ void store_e4m3(uint8_t* p, int col, int cols, const float* f) {
+__device__ __forceinline__ void store_e4m3(uint8_t* p, const float* f) {
     typedef uint32_t u32_b __attribute__((aligned(1)));
     typedef u32x2 u32x2_b __attribute__((aligned(1)));
-    uint32_t w[PER / 4];
-#pragma unroll
-    for (int j = 0; j < PER / 4; ++j)
-        w[j] = pack_e4m3(f + 4 * j);
-    if (col + PER <= cols) {
-        if constexpr (PER == 8)
-            *reinterpret_cast<u32x2_b*>(p + col) = u32x2{w[0], w[1]};
-        else
-            *reinterpret_cast<u32_b*>(p + col) = w[0];
-    } else {
-#pragma unroll
-        for (int j = 0; j < PER; ++j)
-            if (col + j < cols)
-                p[col + j] = (uint8_t)(w[j / 4] >> 8 * (j % 4));
-    }
+    if constexpr (PER == 8)
+        *reinterpret_cast<u32x2_b*>(p) = u32x2{pack_e4m3(f), pack_e4m3(f + 4)};
+    else
+        *reinterpret_cast<u32_b*>(p) = pack_e4m3(f);
 }
 
 // Largest over runs of `lanes` neighbouring lanes (a power of two, 4 to 64, the same in the whole grid).
@@ -73,75 +62,142 @@ __device__ __forceinline__ uint32_t run_max(uint32_t x, int lanes) {
 // A magnitude's bits: they order as the magnitudes, NaN above all.
 __device__ __forceinline__ uint32_t mag_bits(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7FFFFFFFu; }
 
+// How LPR lanes hold a row of `cols` elements: the vector at slot i of a lane is number
+// lane + i * LPR of `full`, and the elements after the last whole vector lie two a lane on the
+// aligned four lanes around the place that a further vector would have, at slot `slot`.  (A run of lanes with
+// one scale is four or more, so it has them.)
+template <typename T, int LPR>
+struct Held {
+    int lane, full, slot, tail[2];  // tail: columns of this lane's odd elements, -1: none
+    __device__ __forceinline__ Held(int lane_, int cols) : lane(lane_), full(cols / T::kPer), slot(full / LPR) {
+        const int from = full * T::kPer, e = lane - (full % LPR & ~3);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int c = from + 2 * e + j;
+            tail[j] = e >= 0 && e < 4 && c < cols ? c : -1;
+        }
+    }
+    __device__ __forceinline__ bool has(int i) const { return lane + i * LPR < full; }
+    __device__ __forceinline__ int column(int i) const { return (lane + i * LPR) * T::kPer; }
+    // calls f(j, column) for this lane's odd elements
+    template <typename F>
+    __device__ __forceinline__ void odd(F f) const {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            if (tail[j] >= 0)
+                f(j, tail[j]);
+    }
+};
+
+// Rows of more than 64 vectors go past the caches: 4096 rows of 1600 f16 9.7 us in place of 11.5,
+// 16384 of 4096 95 in place of 108; rows of 512 lose by it (13.6, 12.7).
+constexpr bool norm_past(int lpr, int nv) { return lpr * nv > 64; }
+
 template <typename T, int LPR, int NV>
 __global__ __launch_bounds__(norm_block(LPR)) void k_rms_norm(const zero_rms_norm_args_t a, int64_t first) {
-    // a run of lanes that shares a scale lies in one vector's lanes, or is all of them
+    // a run of lanes that shares a scale lies in one slot's lanes, or is all of them
     static_assert(LPR >= 64 || NV == 1, "short rows take one vector a lane");
     using elem = typename T::elem;
     constexpr int kPer = T::kPer, kBlock = norm_block(LPR);
+    constexpr bool PAST = norm_past(LPR, NV);
     __shared__ float sums[LPR > 64 ? LPR / 64 : 1];
     __shared__ uint32_t tops[LPR > 64 ? LPR / 64 : 1];
     const int lane = threadIdx.x % LPR, cols = (int)a.cols;
     const int64_t row = first + (int64_t)blockIdx.x * (kBlock / LPR) + threadIdx.x / LPR;
     if (row >= a.rows)
         return;  // whole segments of waves: a workgroup with several rows has no barrier
+    const Held<T, LPR> held(lane, cols);
     const elem* x = static_cast<const elem*>(a.x) + row * a.ld_x;
     const elem* r = static_cast<const elem*>(a.residual) + row * a.ld_residual;
     const elem* w = static_cast<const elem*>(a.weight);
     elem* h = static_cast<elem*>(a.h) + row * a.ld_h;
     elem* y = static_cast<elem*>(a.y) + row * a.ld_y;
 
+    // everything the row needs is on its way before any of it is used
+    u32x4 v[NV], rv[NV], wv[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        v[i] = rv[i] = wv[i] = u32x4{0, 0, 0, 0};
+        if (held.has(i)) {
+            v[i] = load_vec<T, PAST>(x + held.column(i));
+            if (a.residual)
+                rv[i] = load_vec<T, PAST>(r + held.column(i));
+        }
+    }
+    float fo[2] = {}, ro[2] = {}, wo[2] = {};
+    held.odd([&](int j, int c) {
+        fo[j] = T::to_f32(x[c]);
+        if (a.residual)
+            ro[j] = T::to_f32(r[c]);
+        wo[j] = T::to_f32(w[c]);
+    });
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (held.has(i))
+            wv[i] = load_vec<T, false>(w + held.column(i));
+
     float f[NV][kPer];
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (lane + i * LPR) * kPer;
-        u32x4 v = {0, 0, 0, 0};
-        if (c < cols) {
-            v = load_row<T>(x, c, cols, 0);
-            if (a.residual) {
-                float p[kPer], g[kPer];
-                T::unpack(v, p);
-                T::unpack(load_row<T>(r, c, cols, 0), g);
+        T::unpack(v[i], f[i]);
+        if (a.residual) {
+            float g[kPer];
+            T::unpack(rv[i], g);
 #pragma unroll
-                for (int j = 0; j < kPer; ++j)
-                    p[j] += g[j];
-                v = T::pack(p);
-                if (a.h)
-                    store_row<T>(h, c, cols, v);
-            }
+            for (int j = 0; j < kPer; ++j)
+                f[i][j] += g[j];
+            v[i] = T::pack(f[i]);
+            T::unpack(v[i], f[i]);  // the norm is of the rounded sum, which is what the backward reads
+            if (a.h && held.has(i))
+                store_vec<T, PAST>(h + held.column(i), v[i]);
         }
-        T::unpack(v, f[i]);  // the norm is of the rounded sum, which is what the backward reads
 #pragma unroll
         for (int j = 0; j < kPer; ++j)
             sum = __builtin_fmaf(f[i][j], f[i][j], sum);
     }
+    held.odd([&](int j, int c) {
+        if (a.residual) {
+            const elem e = T::of_f32(fo[j] + ro[j]);
+            fo[j] = T::to_f32(e);
+            if (a.h)
+                h[c] = e;
+        }
+        sum = __builtin_fmaf(fo[j], fo[j], sum);
+    });
     sum = row_reduce<LPR>(sum, sums, Add());
     const float rstd = 1.0f / sqrtf(sum / (float)cols + (float)a.eps);
     if (a.rstd && lane == 0)
         a.rstd[row] = rstd;
 
-    uint32_t top[NV];  // the largest |y| of each vector
+    uint32_t top[NV];  // the largest |y| of each slot
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (lane + i * LPR) * kPer;
+        float g[kPer];
+        T::unpack(wv[i], g);
         top[i] = 0;
-        if (c < cols) {
-            float g[kPer];
-            T::unpack(load_row<T>(w, c, cols, 0), g);
+        if (held.has(i)) {  // elsewhere a rstd of inf or NaN would count
 #pragma unroll
             for (int j = 0; j < kPer; ++j) {
                 f[i][j] = f[i][j] * rstd * g[j];
-                if (c + j < cols)  // past the row a rstd of inf or NaN would count
-                    top[i] = MaxU()(top[i], mag_bits(f[i][j]));
+                top[i] = MaxU()(top[i], mag_bits(f[i][j]));
             }
             if (a.y)
-                store_row<T>(y, c, cols, T::pack(f[i]));
+                store_vec<T, PAST>(y + held.column(i), T::pack(f[i]));
         }
     }
+    uint32_t top_odd = 0;
+    held.odd([&](int j, int c) {
+        fo[j] = fo[j] * rstd * wo[j];
+        top_odd = MaxU()(top_odd, mag_bits(fo[j]));
+        if (a.y)
+            y[c] = T::of_f32(fo[j]);
+    });
     if (!a.q8)
         return;
-    uint8_t* q = a.q8 + row * a.ld_q8;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        top[i] = i == held.slot ? MaxU()(top[i], top_odd) : top[i];
     const int group = a.group;
     if (group == 0) {
         uint32_t m = top[0];
@@ -158,134 +214,198 @@ __global__ __launch_bounds__(norm_block(LPR)) void k_rms_norm(const zero_rms_nor
         for (int i = 0; i < NV; ++i)
             top[i] = run_max(top[i], run);
     }
+    uint8_t* q = a.q8 + row * a.ld_q8;
     float* scale = a.scale + row * (group ? (cols + group - 1) / group : 1);
+    auto scale_of = [](uint32_t m) {
+        const float t = __builtin_bit_cast(float, m);
+        return (t < kScaleFloor ? kScaleFloor : t) / kE4m3Max;
+    };
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (lane + i * LPR) * kPer;
-        if (c < cols) {
-            float t = __builtin_bit_cast(float, top[i]);
-            t = (t < kScaleFloor ? kScaleFloor : t) / kE4m3Max;
-            if (group ? c % group == 0 : c == 0)
-                scale[group ? c / group : 0] = t;
+        const int c = held.column(i);
+        const float t = scale_of(top[i]);
+        if (c < cols && (group ? (c & (group - 1)) == 0 : c == 0))
+            scale[group ? c / group : 0] = t;
+        if (held.has(i)) {
             const float inv = 1.0f / t;
             float g[kPer];
 #pragma unroll
             for (int j = 0; j < kPer; ++j)
                 g[j] = f[i][j] * inv;
-            store_e4m3<kPer>(q, c, cols, g);
+            store_e4m3<kPer>(q + c, g);
+        }
+        if (i == held.slot) {
+            held.odd([&](int j, int at) {
+                float g[4] = {fo[j] * (1.0f / t)};
+                q[at] = (uint8_t)pack_e4m3(g);
+            });
         }
     }
 }
 
-// Rows are dealt to the grid's workgroups in turn (a workgroup takes kBlock / LPR at a time); each
-// keeps its rows' sum of dy n in registers, its lanes' columns being the same in every row, and
-// leaves one row of partial sums (`part` [gridDim.x, cols]); where it is the only workgroup it
-// writes dweight itself.
+// Rows are dealt to the grid's workgroups in turn, kRows at a time; each keeps its rows' sum of dy n in
+// registers, its lanes' columns being the same in every row, and leaves one row of partial sums
+// (`part` [gridDim.x, cols]); where it is the only workgroup it writes dweight itself.
+//
+// A row's arrays are loaded while the row before it is worked on (kAhead), where the registers are
+// enough for that; wider rows read dh and the weight as they are needed.
+constexpr int kBackBlock = 1024;
+
 template <typename T, int LPR, int NV>
-__global__ __launch_bounds__(norm_block(LPR)) void k_rms_norm_back(const zero_rms_norm_backward_args_t a,
-                                                                   float* part) {
+__global__ __launch_bounds__(kBackBlock) void k_rms_norm_back(const zero_rms_norm_backward_args_t a, float* part) {
     using elem = typename T::elem;
-    constexpr int kPer = T::kPer, kBlock = norm_block(LPR), kRows = kBlock / LPR;
-    __shared__ float sums[2][LPR > 64 ? LPR / 64 : 1];
+    constexpr int kPer = T::kPer, kBlock = kBackBlock, kRows = kBlock / LPR;
+    constexpr bool PAST = norm_past(LPR, NV), kAhead = NV <= 2;
+    __shared__ float sums[2][kRows][LPR > 64 ? LPR / 64 : 1];
     __shared__ float join[kRows > 1 ? LPR * NV * kPer : 1];
     const int lane = threadIdx.x % LPR, cols = (int)a.cols;
+    const Held<T, LPR> held(lane, cols);
     const elem* w = static_cast<const elem*>(a.weight);
-    float dw[NV][kPer] = {};
+    struct Row {
+        u32x4 h[NV], dy[NV], dh[kAhead ? NV : 1];
+        float rstd;
+    };
+    auto load = [&](Row& q, int64_t row) __attribute__((always_inline)) {
+        const elem* dy = static_cast<const elem*>(a.dy) + row * a.ld_dy;
+        const elem* h = static_cast<const elem*>(a.h) + row * a.ld_h;
+        const elem* dh = static_cast<const elem*>(a.dh) + row * a.ld_dh;
+        const bool there = row < a.rows;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            q.h[i] = q.dy[i] = u32x4{0, 0, 0, 0};
+            if (there && held.has(i)) {
+                q.h[i] = load_vec<T, PAST>(h + held.column(i));
+                q.dy[i] = load_vec<T, PAST>(dy + held.column(i));
+            }
+            if constexpr (kAhead) {
+                q.dh[i] = u32x4{0, 0, 0, 0};
+                if (a.dh && there && held.has(i))
+                    q.dh[i] = load_vec<T, PAST>(dh + held.column(i));
+            }
+        }
+        q.rstd = there ? a.rstd[row] : 0.f;
+    };
+    float dw[NV][kPer] = {}, dwo[2] = {}, wo[2] = {};
+    u32x4 wv[kAhead ? NV : 1];
+    if constexpr (kAhead) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            wv[i] = u32x4{0, 0, 0, 0};
+            if (held.has(i))
+                wv[i] = load_vec<T, false>(w + held.column(i));
+        }
+    }
+    held.odd([&](int j, int c) { wo[j] = T::to_f32(w[c]); });
+    // all segments of a workgroup take their turns together; one whose row lies past the last has zeros
+    const int segment = threadIdx.x / LPR;
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    Row q;
+    load(q, (int64_t)blockIdx.x * kRows + segment);
     int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LPR; row < a.rows;
-         row += (int64_t)gridDim.x * kRows, turn ^= 1) {
+    for (int64_t base = (int64_t)blockIdx.x * kRows; base < a.rows; base += step, turn ^= 1) {
+        const int64_t row = base + segment;
+        const bool there = row < a.rows;
         const elem* dy = static_cast<const elem*>(a.dy) + row * a.ld_dy;
         const elem* h = static_cast<const elem*>(a.h) + row * a.ld_h;
         const elem* dh = static_cast<const elem*>(a.dh) + row * a.ld_dh;
         elem* dx = static_cast<elem*>(a.dx) + row * a.ld_dx;
-        const float rstd = a.rstd[row];
-        u32x4 hv[NV], gv[NV], tv[NV];
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (lane + i * LPR) * kPer;
-            hv[i] = gv[i] = tv[i] = u32x4{0, 0, 0, 0};
-            if (c < cols) {
-                hv[i] = load_row<T>(h, c, cols, 0);
-                gv[i] = load_row<T>(dy, c, cols, 0);
+        float no[2] = {}, go[2] = {}, to[2] = {};
+        if (there)
+            held.odd([&](int j, int c) {
+                no[j] = T::to_f32(h[c]);
+                go[j] = T::to_f32(dy[c]);
                 if (a.dh)
-                    tv[i] = load_row<T>(dh, c, cols, 0);
-            }
-        }
+                    to[j] = T::to_f32(dh[c]);
+            });
+        Row next;
+        if constexpr (kAhead)
+            load(next, row + step);
         float dot = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = (lane + i * LPR) * kPer;
-            if (c < cols) {
+            if (held.has(i)) {  // elsewhere a rstd of inf or NaN would count
                 float n[kPer], g[kPer], k[kPer];
-                T::unpack(hv[i], n);
-                T::unpack(gv[i], g);
-                T::unpack(load_row<T>(w, c, cols, 0), k);
+                T::unpack(q.h[i], n);
+                T::unpack(q.dy[i], g);
+                T::unpack(kAhead ? wv[kAhead ? i : 0] : load_vec<T, false>(w + held.column(i)), k);
 #pragma unroll
                 for (int j = 0; j < kPer; ++j) {
-                    n[j] *= rstd;
+                    n[j] *= q.rstd;
                     dw[i][j] = __builtin_fmaf(g[j], n[j], dw[i][j]);
-                    if (c + j < cols)  // past the row a rstd of inf or NaN would count
-                        dot = __builtin_fmaf(g[j] * k[j], n[j], dot);
+                    dot = __builtin_fmaf(g[j] * k[j], n[j], dot);
                 }
             }
         }
-        const float mean = row_reduce<LPR>(dot, sums[turn], Add()) / (float)cols;
+        held.odd([&](int j, int) {
+            no[j] *= q.rstd;
+            dwo[j] = __builtin_fmaf(go[j], no[j], dwo[j]);
+            go[j] *= wo[j];
+            dot = __builtin_fmaf(go[j], no[j], dot);
+        });
+        const float mean = row_reduce<LPR>(dot, sums[turn][segment], Add()) / (float)cols;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = (lane + i * LPR) * kPer;
-            if (c < cols) {
-                float n[kPer], g[kPer], k[kPer], t[kPer];
-                T::unpack(hv[i], n);
-                T::unpack(gv[i], g);
-                T::unpack(load_row<T>(w, c, cols, 0), k);
-                T::unpack(tv[i], t);
+            keep_packed(q.h[i]);
+            keep_packed(q.dy[i]);
+            if (there && held.has(i)) {
+                float n[kPer], g[kPer], k[kPer], t[kPer] = {};
+                T::unpack(q.h[i], n);
+                T::unpack(q.dy[i], g);
+                T::unpack(kAhead ? wv[kAhead ? i : 0] : load_vec<T, false>(w + held.column(i)), k);
+                if (a.dh)
+                    T::unpack(kAhead ? q.dh[kAhead ? i : 0] : load_vec<T, PAST>(dh + held.column(i)), t);
 #pragma unroll
                 for (int j = 0; j < kPer; ++j) {
-                    const float d = rstd * (g[j] * k[j] - n[j] * rstd * mean);
+                    const float d = q.rstd * (g[j] * k[j] - n[j] * q.rstd * mean);
                     t[j] = a.dh ? d + t[j] : d;
                 }
-                store_row<T>(dx, c, cols, T::pack(t));
+                store_vec<T, PAST>(dx + held.column(i), T::pack(t));
             }
         }
+        if (there)
+            held.odd([&](int j, int c) {
+                const float d = q.rstd * (go[j] - no[j] * mean);
+                dx[c] = T::of_f32(a.dh ? d + to[j] : d);
+            });
+        if constexpr (kAhead)
+            q = next;
+        else
+            load(q, row + step);
     }
     // the workgroup's rows of sums, one after another, in the order of its segments
-    elem* dwo = static_cast<elem*>(a.dweight);
+    elem* out = static_cast<elem*>(a.dweight);
     float* mine = part + (int64_t)blockIdx.x * cols;
     const bool alone = gridDim.x == 1;
+    auto put = [&](int c, float d) {
+        if (alone)
+            out[c] = T::of_f32(d);
+        else
+            mine[c] = d;
+    };
     if constexpr (kRows > 1) {
         for (int s = 0; s < kRows; ++s) {
-            if ((int)threadIdx.x / LPR == s) {
+            if (segment == s) {
+                auto add = [&](int c, float d) { join[c] = s ? join[c] + d : d; };
 #pragma unroll
                 for (int i = 0; i < NV; ++i)
+                    if (held.has(i))
 #pragma unroll
-                    for (int j = 0; j < kPer; ++j) {
-                        const int c = (lane + i * LPR) * kPer + j;
-                        join[c] = s ? join[c] + dw[i][j] : dw[i][j];
-                    }
+                        for (int j = 0; j < kPer; ++j)
+                            add(held.column(i) + j, dw[i][j]);
+                held.odd([&](int j, int c) { add(c, dwo[j]); });
             }
             __syncthreads();
         }
-        for (int c = threadIdx.x; c < cols; c += kBlock) {
-            if (alone)
-                dwo[c] = T::of_f32(join[c]);
-            else
-                mine[c] = join[c];
-        }
+        for (int c = threadIdx.x; c < cols; c += kBlock)
+            put(c, join[c]);
     } else {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (lane + i * LPR) * kPer;
-            if (c < cols) {
-                if (alone) {
-                    store_row<T>(dwo, c, cols, T::pack(dw[i]));
-                } else {
+        for (int i = 0; i < NV; ++i)
+            if (held.has(i))
 #pragma unroll
-                    for (int j = 0; j < kPer; ++j)
-                        if (c + j < cols)
-                            mine[c + j] = dw[i][j];
-                }
-            }
-        }
+                for (int j = 0; j < kPer; ++j)
+                    put(held.column(i) + j, dw[i][j]);
+        held.odd([&](int j, int c) { put(c, dwo[j]); });
     }
 }
 

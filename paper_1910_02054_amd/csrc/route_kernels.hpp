@@ -232,7 +232,9 @@ __global__ __launch_bounds__(kOrderBlock) void k_route_count(const int32_t* inde
         counts[(int64_t)blockIdx.x * (experts + 1) + e] = n[e];
 }
 
-// counts may be NULL where the grid is one workgroup.  run is a multiple of kOrderBlock.
+// counts may be NULL where the grid is one workgroup.  run is a multiple of kOrderBlock, OWN * kOrderBlock
+// at least the keys.
+template <int OWN>
 __global__ __launch_bounds__(kOrderBlock) void k_route_order(const int32_t* index, int64_t slots, int experts,
                                                              int64_t run, const int32_t* counts, int32_t* offsets,
                                                              int32_t* order) {
@@ -250,14 +252,14 @@ __global__ __launch_bounds__(kOrderBlock) void k_route_order(const int32_t* inde
     __syncthreads();
 
     // this thread's keys: all slots of each, and those of the workgroups before this one
-    int32_t all[kOrderOwn], prior[kOrderOwn], mine = 0;
+    int32_t all[OWN], prior[OWN], mine = 0;
 #pragma unroll
-    for (int j = 0; j < kOrderOwn; ++j) {
-        const int e = threadIdx.x * kOrderOwn + j;
+    for (int j = 0; j < OWN; ++j) {
+        const int e = threadIdx.x * OWN + j;
         all[j] = prior[j] = 0;
         if (e < keys) {
             if (counts) {
-#pragma unroll 8
+#pragma unroll 16
                 for (unsigned b = 0; b < gridDim.x; ++b) {
                     const int32_t c = counts[(int64_t)b * keys + e];
                     all[j] += c;
@@ -284,8 +286,8 @@ __global__ __launch_bounds__(kOrderBlock) void k_route_order(const int32_t* inde
     for (int w = 0; w < wave; ++w)
         at += sums[w];
 #pragma unroll
-    for (int j = 0; j < kOrderOwn; ++j) {
-        const int e = threadIdx.x * kOrderOwn + j;
+    for (int j = 0; j < OWN; ++j) {
+        const int e = threadIdx.x * OWN + j;
         if (e < keys) {
             if (blockIdx.x == 0)
                 offsets[e] = at;  // of the last key: the slots that have an expert

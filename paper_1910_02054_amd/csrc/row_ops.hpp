@@ -117,10 +117,10 @@ __device__ __forceinline__ void store_vec(typename T::elem* p, u32x4 v) {
 
 // The 16 bytes of row `p` from column `col`, elements at or past `cols` filled from
 // `fill` (a word of two or one of them).
-template <typename T>
+template <typename T, bool NT = false>
 __device__ __forceinline__ u32x4 load_row(const typename T::elem* p, int col, int cols, uint32_t fill) {
     if (col + T::kPer <= cols)
-        return load_vec<T, false>(p + col);
+        return load_vec<T, NT>(p + col);
     u32x4 v = {fill, fill, fill, fill};
     if constexpr (T::kPer == 4) {
 #pragma unroll
@@ -182,6 +182,10 @@ struct Cut {
     __device__ __forceinline__ int edge_column(int e) const { return e < head ? e : tail + e - head; }
 };
 
+// Keeps a packed vector in its registers between two passes over it: without it the compiler holds
+// the first pass's fp32 values for the second, at twice the registers or more.
+__device__ __forceinline__ void keep_packed(u32x4& v) { asm volatile("" : "+v"(v)); }
+
 // ---------------------------------------------------------------------------
 // Reductions.  Steps within rows of 16 lanes by DPP, across them by gfx950's row and
 // half-wave swaps (as zs::wave_sum); every lane of a segment ends with the same bits.
@@ -228,9 +232,9 @@ struct MaxU {
     __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return a > b ? a : b; }
 };
 
-// op over the LANES lanes that share a row; where they are more than a wave, the
-// workgroup is one row's and `lds` (LANES / 64 words of this reduction's own, or last
-// read before the workgroup's latest barrier) carries the waves' values.
+// op over the LANES lanes that share a row.  Where they are more than a wave, `lds` (LANES / 64 words,
+// the row's own, last read before the workgroup's latest barrier) carries the waves' values and
+// all of the workgroup's threads call this together.
 template <int LANES, typename V, typename OP>
 __device__ __forceinline__ V row_reduce(V x, V* lds, OP op) {
     if constexpr (LANES <= 64) {
@@ -239,7 +243,7 @@ __device__ __forceinline__ V row_reduce(V x, V* lds, OP op) {
         constexpr int kWaves = LANES / 64;
         x = seg_reduce<64>(x, op);
         if ((threadIdx.x & 63) == 0)
-            lds[threadIdx.x / 64] = x;
+            lds[threadIdx.x % LANES / 64] = x;
         __syncthreads();
         return seg_reduce<kWaves>(lds[threadIdx.x % kWaves], op);
     }
