@@ -155,15 +155,14 @@ __global__ __launch_bounds__(kRouteBlock) void k_route(const zero_route_args_t a
         const bool has = m == top && top != 0;
         const uint64_t who = __ballot(has);
         if (has && (who & before) == 0) {
-            bool open = true;
+            int at = 0;
 #pragma unroll
-            for (int j = 0; j < VPL; ++j) {
-                const bool hit = open && key[j] == top;
-                if (hit)
-                    chosen[token][i] = from + j;
-                key[j] = hit ? 0u : key[j];
-                open = open && !hit;
-            }
+            for (int j = VPL - 1; j >= 0; --j)
+                at = key[j] == top ? j : at;
+            chosen[token][i] = from + at;
+#pragma unroll
+            for (int j = 0; j < VPL; ++j)
+                key[j] = at == j ? 0u : key[j];
         }
     }
     __syncthreads();
@@ -225,6 +224,7 @@ __global__ __launch_bounds__(kOrderBlock) void k_route_count(const int32_t* inde
         n[e] = 0;
     __syncthreads();
     const int64_t from = blockIdx.x * run, end = from + run < slots ? from + run : slots;
+#pragma unroll 4
     for (int64_t s = from + threadIdx.x; s < end; s += kOrderBlock)
         atomicAdd(&n[slot_key(index, s, experts)], 1);
     __syncthreads();
@@ -247,8 +247,17 @@ __global__ __launch_bounds__(kOrderBlock) void k_route_order(const int32_t* inde
     for (int e = threadIdx.x; e < kOrderWaves * keys; e += kOrderBlock)
         place[e / keys][e % keys] = 0;
     __syncthreads();
-    for (int64_t s = from + lane; s < end; s += 64)
-        atomicAdd(&place[wave][slot_key(index, s, experts)], 1);
+    constexpr int kBatch = 4;  // keys under way at a time
+    for (int64_t s0 = from + lane; s0 < end; s0 += 64 * kBatch) {
+        int key[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+            key[i] = s0 + 64 * i < end ? slot_key(index, s0 + 64 * i, experts) : -1;
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+            if (key[i] >= 0)
+                atomicAdd(&place[wave][key[i]], 1);
+    }
     __syncthreads();
 
     // this thread's keys: all slots of each, and those of the workgroups before this one
@@ -304,22 +313,30 @@ __global__ __launch_bounds__(kOrderBlock) void k_route_order(const int32_t* inde
     __syncthreads();
 
     const int bits = 32 - __builtin_clz(keys);
-    for (int64_t s0 = from; s0 < end; s0 += 64) {
-        const int64_t s = s0 + lane;
-        const int e = s < end ? slot_key(index, s, experts) : 0;
-        uint64_t same = __ballot(s < end);  // lanes with this lane's key
-        for (int i = 0; i < bits; ++i) {
-            const bool bit = e >> i & 1;
-            const uint64_t m = __ballot(bit);
-            same &= bit ? m : ~m;
+    for (int64_t s0 = from; s0 < end; s0 += 64 * kBatch) {
+        int key[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int64_t s = s0 + 64 * i + lane;
+            key[i] = s < end ? slot_key(index, s, experts) : -1;
         }
-        const int rank = __popcll(same & (((uint64_t)1 << lane) - 1));
-        int32_t base = 0;
-        if (s < end && rank == 0)
-            base = atomicAdd(&place[wave][e], (int)__popcll(same));
-        base = __shfl(base, s < end ? __ffsll((unsigned long long)same) - 1 : lane);
-        if (s < end)
-            order[base + rank] = e < experts ? (int32_t)s : -1;
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int e = key[i];
+            uint64_t same = __ballot(e >= 0);  // lanes with this lane's key
+            for (int b = 0; b < bits; ++b) {
+                const bool bit = e >> b & 1;
+                const uint64_t m = __ballot(bit);
+                same &= bit ? m : ~m;
+            }
+            const int rank = __popcll(same & (((uint64_t)1 << lane) - 1));
+            int32_t base = 0;
+            if (e >= 0 && rank == 0)
+                base = atomicAdd(&place[wave][e], (int)__popcll(same));
+            base = __shfl(base, e >= 0 ? __ffsll((unsigned long long)same) - 1 : lane);
+            if (e >= 0)
+                order[base + rank] = e < experts ? (int32_t)(s0 + 64 * i + lane) : -1;
+        }
     }
 }
 

@@ -8,7 +8,6 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
-#include <cstdlib>
 
 #include "host_common.hpp"
 #include "zero_operators.h"
@@ -115,13 +114,30 @@ struct Arrays {
         HIP_TRY(hipStreamIsCapturing(stream, &cap));
         if (cap != hipStreamCaptureStatusNone)
             return ZERO_OK;
-        const void* ptrs[kMost];
-        size_t bytes[kMost];
+        // an allocation that one array has been found in is not looked up again for the next
+        uintptr_t base[kMost], end[kMost];
+        int found = 0;
         for (int i = 0; i < n; ++i) {
-            ptrs[i] = m[i].p;
-            bytes[i] = m[i].bytes();
+            const uintptr_t p = reinterpret_cast<uintptr_t>(m[i].p), e = p + m[i].bytes();
+            int k = 0;
+            while (k < found && !(p >= base[k] && e <= end[k]))
+                ++k;
+            if (k < found)
+                continue;
+            hipDeviceptr_t b = nullptr;
+            size_t size = 0;
+            if (hipMemGetAddressRange(&b, &size, const_cast<void*>(m[i].p)) != hipSuccess || !b) {
+                (void)hipGetLastError();
+                return fail(ZERO_EINVAL, "%s: %s is not in GPU-accessible memory", fn, m[i].name);
+            }
+            base[found] = reinterpret_cast<uintptr_t>(b);
+            end[found] = base[found] + size;
+            if (p < base[found] || e > end[found])
+                return fail(ZERO_EINVAL, "%s: %s ([%p, +%zu B)) overruns its allocation ([%p, +%zu B))", fn, m[i].name,
+                            m[i].p, m[i].bytes(), b, size);
+            ++found;
         }
-        return check_ranges(fn, ptrs, bytes, n);
+        return ZERO_OK;
     }
 };
 
@@ -225,25 +241,31 @@ int with_keys(int64_t need, F f) {
 
 int log2_of(int pow2) { return __builtin_ctz((unsigned)pow2); }
 
-// Lanes of a token: at least one a group and one a slot, and few enough keys a lane.
+// Lanes of a token: at least one a group and one a slot, and few enough keys a lane.  A round of the
+// choice costs a few steps across the lanes and an operation for each key of a lane, and the
+// tokens of a wave share them: up to 8 keys a lane (16384 tokens of 256 experts, 8 of them: 14.5 us, 18.2
+// with 4 keys), up to 16 where a token would take a whole wave otherwise (32768 of 384, 10 of them: 41
+// us, 46 with 8).
 int token_lanes(int experts, int k, int groups) {
     const int g = pow2_up(groups), size = experts / groups;
     int lanes = std::max({8, pow2_up(k), g});
-    static const int most = std::getenv("ZO_VPL") ? std::atoi(std::getenv("ZO_VPL")) : 8;
-    while (lanes < 64 && div_up(size, lanes / g) > most)
+    while (lanes < 64 && div_up(size, lanes / g) > (lanes < 32 ? 8 : 16))
         lanes *= 2;
     return lanes;
 }
 
-const int64_t kOrderRun = std::getenv("ZO_RUN") ? std::atoi(std::getenv("ZO_RUN")) : 2048;     // slots a workgroup of the ordering aims at
+// Slots that a workgroup of the ordering aims at: with few, more workgroups (24594 slots of 60 experts: 9.5
+// us with 1024, 10.9 with 2048); with many, fewer counts that each has to read (131072 of 256: 11.4 and 10.2).
 constexpr int64_t kOrderMaxBlocks = 256;
+
+int64_t order_run(int64_t slots) { return slots < 65536 && slots > 2048 ? 1024 : 2048; }
 
 struct OrderPlan {
     int64_t blocks, run;
 };
 
 OrderPlan order_plan(int64_t slots) {
-    int64_t blocks = std::max<int64_t>(1, std::min(kOrderMaxBlocks, div_up(slots, kOrderRun)));
+    int64_t blocks = std::max<int64_t>(1, std::min(kOrderMaxBlocks, div_up(slots, order_run(slots))));
     const int64_t run = std::max<int64_t>(1, div_up(div_up(slots, blocks), zo::kOrderBlock)) * zo::kOrderBlock;
     blocks = std::max<int64_t>(1, div_up(slots, run));
     return OrderPlan{blocks, run};

@@ -9,61 +9,28 @@ dimensions are taken as one where their strides allow it, else the rows may be a
 apart.
 """
 import ctypes
+import struct
 
 import torch
 
-from .binding import ZeroError, _addr, _check, _lib, _stream  # noqa: F401
+from .binding import ZeroError, _check, _lib, _stream  # noqa: F401
 
 ZERO_F32, ZERO_F16, ZERO_BF16 = 0, 1, 2
 ZERO_SCORE_SOFTMAX, ZERO_SCORE_SIGMOID = 0, 1
 _TYPE = {torch.float32: ZERO_F32, torch.float16: ZERO_F16, torch.bfloat16: ZERO_BF16}
 _SCORE = {"softmax": ZERO_SCORE_SOFTMAX, "sigmoid": ZERO_SCORE_SIGMOID}
-_Q8 = (torch.float8_e4m3fn, torch.uint8)
 
 _P, _i64, _i32, _dbl = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_double
 
 
-class RmsNormArgs(ctypes.Structure):
-    """Mirror of zero_rms_norm_args_t."""
-    _fields_ = [("dtype", _i32), ("group", _i32), ("rows", _i64), ("cols", _i64), ("eps", _dbl), ("x", _P),
-                ("ld_x", _i64), ("residual", _P), ("ld_residual", _i64), ("weight", _P), ("h", _P), ("ld_h", _i64),
-                ("y", _P), ("ld_y", _i64), ("q8", _P), ("ld_q8", _i64), ("scale", _P), ("rstd", _P)]
-
-
-class RmsNormBackwardArgs(ctypes.Structure):
-    """Mirror of zero_rms_norm_backward_args_t."""
-    _fields_ = [("dtype", _i32), ("pad_", _i32), ("rows", _i64), ("cols", _i64), ("dy", _P), ("ld_dy", _i64),
-                ("h", _P), ("ld_h", _i64), ("weight", _P), ("rstd", _P), ("dh", _P), ("ld_dh", _i64), ("dx", _P),
-                ("ld_dx", _i64), ("dweight", _P), ("workspace", _P), ("workspace_floats", _i64)]
-
-
-class RouteArgs(ctypes.Structure):
-    """Mirror of zero_route_args_t."""
-    _fields_ = [("dtype", _i32), ("score", _i32), ("rows", _i64), ("experts", _i32), ("k", _i32), ("groups", _i32),
-                ("top_groups", _i32), ("group_top", _i32), ("renormalise", _i32), ("scale", _dbl), ("logits", _P),
-                ("ld_logits", _i64), ("bias", _P), ("index", _P), ("weight", _P)]
-
-
-class RouteOrderArgs(ctypes.Structure):
-    """Mirror of zero_route_order_args_t."""
-    _fields_ = [("index", _P), ("slots", _i64), ("experts", _i32), ("pad_", _i32), ("offsets", _P), ("order", _P),
-                ("workspace", _P), ("workspace_ints", _i64)]
-
-
-class RouteBackwardArgs(ctypes.Structure):
-    """Mirror of zero_route_backward_args_t."""
-    _fields_ = [("dtype", _i32), ("score", _i32), ("rows", _i64), ("experts", _i32), ("k", _i32),
-                ("renormalise", _i32), ("pad_", _i32), ("scale", _dbl), ("logits", _P), ("ld_logits", _i64),
-                ("bias", _P), ("index", _P), ("dweight", _P), ("dlogits", _P), ("ld_dlogits", _i64)]
-
-
-class DistillArgs(ctypes.Structure):
-    """Mirror of zero_distill_args_t."""
-    _fields_ = [("dtype", _i32), ("teacher_dtype", _i32), ("rows", _i64), ("vocab", _i64), ("k", _i32),
-                ("pad_", _i32), ("temperature", _dbl), ("soft", _dbl), ("hard", _dbl), ("grad_scale", _dbl),
-                ("logits", _P), ("ld_logits", _i64), ("teacher_index", _P), ("teacher_logits", _P), ("labels", _P),
-                ("row_weight", _P), ("loss", _P), ("stats", _P), ("dloss", _P), ("dlogits", _P), ("ld_dlogits", _i64)]
-
+# The argument records of the C ABI (zero_rms_norm_args_t and so on), their fields in order: packed
+# into bytes for the call, which takes half the time of filling a ctypes.Structure of that many fields.
+RMS_NORM_ARGS = struct.Struct("@iiqqdPqPqPPqPqPqPP")
+RMS_NORM_BACKWARD_ARGS = struct.Struct("@iiqqPqPqPPPqPqPPq")
+ROUTE_ARGS = struct.Struct("@iiqiiiiiidPqPPP")
+ROUTE_ORDER_ARGS = struct.Struct("@PqiiPPPq")
+ROUTE_BACKWARD_ARGS = struct.Struct("@iiqiiiidPqPPPPq")
+DISTILL_ARGS = struct.Struct("@iiqqiiddddPqPPPPPPPPq")
 
 EXPORTS = ("zero_rms_norm", "zero_rms_norm_backward", "zero_rms_norm_workspace", "zero_route", "zero_route_order",
            "zero_route_workspace", "zero_route_backward", "zero_distill_step", "zero_distill_loss",
@@ -75,46 +42,74 @@ _lib.zero_rms_norm_workspace.argtypes = [_i64, _i64, ctypes.POINTER(_i64)]
 _lib.zero_route_workspace.argtypes = [_i64, _i32, ctypes.POINTER(_i64)]
 
 
-def _matrix(t, dtypes, what, rows=None, cols=None):
-    """(address, rows, cols, elements from row to row) of a device matrix; None gives no address."""
+_raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+
+def _on(stream):
+    """The hipStream_t of `stream`, or of torch's current stream on the current device."""
+    return _raw_stream(_device()) if stream is None else _stream(stream)
+
+
+def _type(t, what):
+    code = _TYPE.get(t.dtype)
+    if code is None:
+        raise TypeError("%s: dtype %s not in %s" % (what, t.dtype, tuple(_TYPE)))
+    return code
+
+
+def _sizes(t, what):
+    """(rows, columns) of a matrix whose leading dimensions count as one."""
+    shape = t.shape
+    if len(shape) == 2:
+        return shape
+    if not shape:
+        raise ValueError("%s must have a dimension" % what)
+    n = shape[-1]
+    return (t.numel() // n if n else 0), n
+
+
+def _matrix(t, dtype, what, rows, cols):
+    """(address, elements from row to row) of a device matrix of the given type and size; (0, cols) for None."""
     if t is None:
-        return None, rows, cols, cols
-    if t.dtype not in dtypes:
-        raise TypeError("%s: dtype %s not in %s" % (what, t.dtype, dtypes))
+        return 0, cols
+    if t.dtype is not dtype:
+        raise TypeError("%s: dtype %s, not %s" % (what, t.dtype, dtype))
     if not t.is_cuda:
         raise TypeError("%s must be a device tensor" % what)
-    if t.dim() != 2:
-        if t.dim() < 1:
-            raise ValueError("%s must have a dimension" % what)
-        t = t.view(-1, t.shape[-1]) if t.numel() else t.reshape(0, t.shape[-1])
-    n, c = t.shape
-    if (rows is not None and n != rows) or (cols is not None and c != cols):
-        raise ValueError("%s has shape [%d, %d], not [%s, %s]" % (what, n, c, rows, cols))
+    shape = t.shape
+    if len(shape) != 2:
+        t = t.view(-1, shape[-1]) if t.numel() else t.reshape(0, shape[-1])
+        shape = t.shape
+    n, c = shape
+    if n != rows or c != cols:
+        raise ValueError("%s has shape [%d, %d], not [%d, %d]" % (what, n, c, rows, cols))
     step, one = t.stride()
     if one != 1 and c > 1 and n > 0:
         raise ValueError("%s: the last dimension must be contiguous" % what)
-    return t.data_ptr(), n, c, step if n > 1 else c
+    return t.data_ptr(), step if n > 1 else c
 
 
-def _vector(t, dtypes, what, numel):
-    """The address of a contiguous device array of `numel` elements (None gives none)."""
-    if t is not None and t.numel() != numel:
+def _vector(t, dtype, what, numel):
+    """The address of a contiguous device array of `numel` elements (0 for None)."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype:
+        raise TypeError("%s: dtype %s, not %s" % (what, t.dtype, dtype))
+    if not t.is_cuda:
+        raise TypeError("%s must be a device tensor" % what)
+    if not t.is_contiguous():
+        raise TypeError("%s must be contiguous" % what)
+    if t.numel() != numel:
         raise ValueError("%s has %d elements, not %d" % (what, t.numel(), numel))
-    return _addr(t, dtypes, what)
+    return t.data_ptr()
 
 
 def _room(t, dtype, what):
     """(address, elements) of a workspace, which may be None."""
-    return (None, 0) if t is None else (_addr(t, (dtype,), what), t.numel())
+    return (0, 0) if t is None else (_vector(t, dtype, what, t.numel()), t.numel())
 
 
-_F32, _I32 = (torch.float32,), (torch.int32,)
-
-
-def _types(t, what):
-    if t.dtype not in _TYPE:
-        raise TypeError("%s: dtype %s not in %s" % (what, t.dtype, tuple(_TYPE)))
-    return (t.dtype,)
+_F32, _I32 = torch.float32, torch.int32
 
 
 def zero_rms_norm(x, weight, eps, residual=None, h=None, y=None, q8=None, scale=None, group=0, rstd=None,
@@ -123,17 +118,22 @@ def zero_rms_norm(x, weight, eps, residual=None, h=None, y=None, q8=None, scale=
     rows y in e4m3 (torch.float8_e4m3fn or uint8 codes) with one fp32 scale for each `group` columns (0: a row).
     Each output is written where a tensor is given; y, q8 * scale and h are [rows, cols], rstd [rows],
     scale [rows, ceil(cols / group)].  h may be residual or x in place, and so may y."""
-    dt = _types(x, "x")
-    px, rows, cols, ld_x = _matrix(x, dt, "x")
-    pr, _, _, ld_r = _matrix(residual, dt, "residual", rows, cols)
-    ph, _, _, ld_h = _matrix(h, dt, "h", rows, cols)
-    py, _, _, ld_y = _matrix(y, dt, "y", rows, cols)
-    pq, _, _, ld_q = _matrix(q8, _Q8, "q8", rows, cols)
-    groups = -(-cols // group) if group > 0 else 1
-    args = RmsNormArgs(_TYPE[x.dtype], group, rows, cols, eps, px, ld_x, pr, ld_r, _vector(weight, dt, "weight", cols),
-                       ph, ld_h, py, ld_y, pq, ld_q, _vector(scale, _F32, "scale", rows * groups),
-                       _vector(rstd, _F32, "rstd", rows))
-    _check(_lib.zero_rms_norm(ctypes.addressof(args), _stream(stream)))
+    code, dt = _type(x, "x"), x.dtype
+    rows, cols = _sizes(x, "x")
+    px, ld_x = _matrix(x, dt, "x", rows, cols)
+    pr, ld_r = _matrix(residual, dt, "residual", rows, cols)
+    ph, ld_h = _matrix(h, dt, "h", rows, cols)
+    py, ld_y = _matrix(y, dt, "y", rows, cols)
+    pq, ld_q, ps = 0, cols, 0
+    if q8 is not None:
+        pq, ld_q = _matrix(q8, torch.uint8 if q8.dtype is torch.uint8 else torch.float8_e4m3fn, "q8", rows, cols)
+    if scale is not None:
+        ps = _vector(scale, _F32, "scale", rows * (-(-cols // group) if group > 0 else 1))
+    args = RMS_NORM_ARGS.pack(code, group, rows, cols, eps, px, ld_x, pr, ld_r, _vector(weight, dt, "weight", cols), ph, ld_h,
+                       py, ld_y, pq, ld_q, ps, _vector(rstd, _F32, "rstd", rows))
+    rc = _lib.zero_rms_norm(args, _on(stream))
+    if rc < 0:
+        _check(rc)
 
 
 def zero_rms_norm_workspace(rows, cols):
@@ -148,16 +148,26 @@ def zero_rms_norm_backward(dy, h, weight, rstd, dx, dweight, workspace=None, dh=
     place) and dweight [cols], from dy, the h and rstd of the forward (h is x where it had no residual) and the
     gradient dh that reaches h from elsewhere.  workspace: a float32 tensor of at least
     zero_rms_norm_workspace(rows, cols) elements."""
-    dt = _types(h, "h")
-    ph, rows, cols, ld_h = _matrix(h, dt, "h")
-    pdy, _, _, ld_dy = _matrix(dy, dt, "dy", rows, cols)
-    pdh, _, _, ld_dh = _matrix(dh, dt, "dh", rows, cols)
-    pdx, _, _, ld_dx = _matrix(dx, dt, "dx", rows, cols)
-    pw, n = _room(workspace, torch.float32, "workspace")
-    args = RmsNormBackwardArgs(_TYPE[h.dtype], 0, rows, cols, pdy, ld_dy, ph, ld_h,
-                               _vector(weight, dt, "weight", cols), _vector(rstd, _F32, "rstd", rows), pdh, ld_dh,
-                               pdx, ld_dx, _vector(dweight, dt, "dweight", cols), pw, n)
-    _check(_lib.zero_rms_norm_backward(ctypes.addressof(args), _stream(stream)))
+    code, dt = _type(h, "h"), h.dtype
+    rows, cols = _sizes(h, "h")
+    ph, ld_h = _matrix(h, dt, "h", rows, cols)
+    pdy, ld_dy = _matrix(dy, dt, "dy", rows, cols)
+    pdh, ld_dh = _matrix(dh, dt, "dh", rows, cols)
+    pdx, ld_dx = _matrix(dx, dt, "dx", rows, cols)
+    pw, n = _room(workspace, _F32, "workspace")
+    args = RMS_NORM_BACKWARD_ARGS.pack(code, 0, rows, cols, pdy, ld_dy, ph, ld_h, _vector(weight, dt, "weight", cols),
+                               _vector(rstd, _F32, "rstd", rows), pdh, ld_dh, pdx, ld_dx,
+                               _vector(dweight, dt, "dweight", cols), pw, n)
+    rc = _lib.zero_rms_norm_backward(args, _on(stream))
+    if rc < 0:
+        _check(rc)
+
+
+def _score(score):
+    code = _SCORE.get(score)
+    if code is None:
+        raise ValueError("score must be one of %s" % (tuple(_SCORE),))
+    return code
 
 
 def zero_route(logits, index, weight, score="softmax", bias=None, groups=1, top_groups=1, group_top=1,
@@ -165,15 +175,16 @@ def zero_route(logits, index, weight, score="softmax", bias=None, groups=1, top_
     """The choice of k experts for each row of logits [tokens, experts]: index (int32) and weight (float32), both
     [tokens, k], in falling order of the keys.  score: "softmax" or "sigmoid"; bias [experts] float32 acts on the
     choice alone; groups > 1 keeps the top_groups groups of the largest sums of their group_top largest keys."""
-    dt = _types(logits, "logits")
-    pl, rows, experts, ld = _matrix(logits, dt, "logits")
+    code = _type(logits, "logits")
+    rows, experts = _sizes(logits, "logits")
+    pl, ld = _matrix(logits, logits.dtype, "logits", rows, experts)
     k = index.shape[-1]
-    if score not in _SCORE:
-        raise ValueError("score must be one of %s" % (tuple(_SCORE),))
-    args = RouteArgs(_TYPE[logits.dtype], _SCORE[score], rows, experts, k, groups, top_groups, group_top,
-                     bool(renormalise), scale, pl, ld, _vector(bias, _F32, "bias", experts),
-                     _vector(index, _I32, "index", rows * k), _vector(weight, _F32, "weight", rows * k))
-    _check(_lib.zero_route(ctypes.addressof(args), _stream(stream)))
+    args = ROUTE_ARGS.pack(code, _score(score), rows, experts, k, groups, top_groups, group_top, bool(renormalise), scale,
+                     pl, ld, _vector(bias, _F32, "bias", experts), _vector(index, _I32, "index", rows * k),
+                     _vector(weight, _F32, "weight", rows * k))
+    rc = _lib.zero_route(args, _on(stream))
+    if rc < 0:
+        _check(rc)
 
 
 def zero_route_workspace(slots, experts):
@@ -188,44 +199,50 @@ def zero_route_order(index, experts, offsets, order, workspace=None, stream=None
     expert e's; slots without an expert are left out and order ends in as many -1.  offsets [experts + 1] and order
     [slots] are int32; workspace: int32, at least zero_route_workspace(slots, experts) elements."""
     n = index.numel()
-    pw, room = _room(workspace, torch.int32, "workspace")
-    args = RouteOrderArgs(_addr(index, _I32, "index"), n, experts, 0,
+    pw, room = _room(workspace, _I32, "workspace")
+    args = ROUTE_ORDER_ARGS.pack(_vector(index, _I32, "index", n), n, experts, 0,
                           _vector(offsets, _I32, "offsets", experts + 1), _vector(order, _I32, "order", n), pw, room)
-    _check(_lib.zero_route_order(ctypes.addressof(args), _stream(stream)))
+    rc = _lib.zero_route_order(args, _on(stream))
+    if rc < 0:
+        _check(rc)
 
 
 def zero_route_backward(logits, index, dweight, dlogits, score="softmax", bias=None, renormalise=True, scale=1.0,
                         stream=None):
     """The gradient of zero_route's logits into dlogits [tokens, experts] (may be logits in place) from that of its
     weights, dweight [tokens, k] float32, and its index."""
-    dt = _types(logits, "logits")
-    pl, rows, experts, ld = _matrix(logits, dt, "logits")
-    pd, _, _, ld_d = _matrix(dlogits, dt, "dlogits", rows, experts)
+    code, dt = _type(logits, "logits"), logits.dtype
+    rows, experts = _sizes(logits, "logits")
+    pl, ld = _matrix(logits, dt, "logits", rows, experts)
+    pd, ld_d = _matrix(dlogits, dt, "dlogits", rows, experts)
     k = index.shape[-1]
-    if score not in _SCORE:
-        raise ValueError("score must be one of %s" % (tuple(_SCORE),))
-    args = RouteBackwardArgs(_TYPE[logits.dtype], _SCORE[score], rows, experts, k, bool(renormalise), 0, scale, pl,
-                             ld, _vector(bias, _F32, "bias", experts), _vector(index, _I32, "index", rows * k),
+    args = ROUTE_BACKWARD_ARGS.pack(code, _score(score), rows, experts, k, bool(renormalise), 0, scale, pl, ld,
+                             _vector(bias, _F32, "bias", experts), _vector(index, _I32, "index", rows * k),
                              _vector(dweight, _F32, "dweight", rows * k), pd, ld_d)
-    _check(_lib.zero_route_backward(ctypes.addressof(args), _stream(stream)))
+    rc = _lib.zero_route_backward(args, _on(stream))
+    if rc < 0:
+        _check(rc)
 
 
 def _distill(fn, logits, teacher_index, teacher_logits, loss, stats, dlogits, dloss, labels, soft, hard, temperature,
              row_weight, grad_scale, stream):
-    dt = _types(logits, "logits")
-    pl, rows, vocab, ld = _matrix(logits, dt, "logits")
-    pd, _, _, ld_d = _matrix(dlogits, dt, "dlogits", rows, vocab)
-    k = 0 if teacher_index is None else teacher_index.shape[-1]
-    teacher = ZERO_F32
-    if k:
-        teacher = _TYPE[_types(teacher_logits, "teacher_logits")[0]]
-    args = DistillArgs(_TYPE[logits.dtype], teacher, rows, vocab, k, 0, temperature, soft, hard, grad_scale, pl, ld,
-                       _vector(teacher_index, _I32, "teacher_index", rows * k),
-                       _vector(teacher_logits, None, "teacher_logits", rows * k),
+    code, dt = _type(logits, "logits"), logits.dtype
+    rows, vocab = _sizes(logits, "logits")
+    pl, ld = _matrix(logits, dt, "logits", rows, vocab)
+    pd, ld_d = _matrix(dlogits, dt, "dlogits", rows, vocab)
+    k, teacher, pi, pt = 0, ZERO_F32, 0, 0
+    if teacher_index is not None:
+        k = teacher_index.shape[-1]
+        teacher = _type(teacher_logits, "teacher_logits")
+        pi = _vector(teacher_index, _I32, "teacher_index", rows * k)
+        pt = _vector(teacher_logits, teacher_logits.dtype, "teacher_logits", rows * k)
+    args = DISTILL_ARGS.pack(code, teacher, rows, vocab, k, 0, temperature, soft, hard, grad_scale, pl, ld, pi, pt,
                        _vector(labels, _I32, "labels", rows), _vector(row_weight, _F32, "row_weight", rows),
                        _vector(loss, _F32, "loss", rows), _vector(stats, _F32, "stats", 3 * rows),
                        _vector(dloss, _F32, "dloss", rows), pd, ld_d)
-    _check(fn(ctypes.addressof(args), _stream(stream)))
+    rc = fn(args, _on(stream))
+    if rc < 0:
+        _check(rc)
 
 
 def zero_distill_step(logits, teacher_index, teacher_logits, loss, dlogits, labels=None, soft=1.0, hard=0.0,
