@@ -232,8 +232,8 @@ def distill(z, index, teacher, labels, soft, hard, tau, weight, scale, dloss=Non
         off = off + torch.where(has, abs(hard) * (l.abs() + 1) * (units.gather(1, at) + 8 * U), 0.0)[:, 0]
         g = g + torch.where(has, hard * lq.exp(), 0.0)
         gb = gb + torch.where(has, abs(hard) * (lq.exp() * units + NORMAL), 0.0)
-        g = g.scatter_add(1, at, torch.where(has, -hard, 0.0).double())
-        gb = gb.scatter_add(1, at, torch.where(has, abs(hard) * 4 * U, 0.0).double())
+        g = g.scatter_add(1, at, has.double() * -hard)
+        gb = gb.scatter_add(1, at, has.double() * (abs(hard) * 4 * U))
     seen = weight != 0
     loss = torch.where(seen, weight * loss, 0.0)
     off = torch.where(seen, weight.abs() * off, 0.0) + 2 * U * loss.abs()
