@@ -65,28 +65,26 @@ def _sizes(t, what):
     if not shape:
         raise ValueError("%s must have a dimension" % what)
     n = shape[-1]
-    return (t.numel() // n if n else 0), n
+    return torch.Size((t.numel() // n if n else 0, n))
 
 
-def _matrix(t, dtype, what, rows, cols):
+def _matrix(t, dtype, what, size):
     """(address, elements from row to row) of a device matrix of the given type and size; (0, cols) for None."""
     if t is None:
-        return 0, cols
+        return 0, size[1]
     if t.dtype is not dtype:
         raise TypeError("%s: dtype %s, not %s" % (what, t.dtype, dtype))
     if not t.is_cuda:
         raise TypeError("%s must be a device tensor" % what)
-    shape = t.shape
-    if len(shape) != 2:
-        t = t.view(-1, shape[-1]) if t.numel() else t.reshape(0, shape[-1])
-        shape = t.shape
-    n, c = shape
-    if n != rows or c != cols:
-        raise ValueError("%s has shape [%d, %d], not [%d, %d]" % (what, n, c, rows, cols))
+    if t.shape != size:
+        if _sizes(t, what) != size:
+            raise ValueError("%s has shape %s, not %s" % (what, list(t.shape), list(size)))
+        t = t.view(size) if t.numel() else t.reshape(size)
     step, one = t.stride()
-    if one != 1 and c > 1 and n > 0:
+    rows, cols = size
+    if one != 1 and cols > 1 and rows > 0:
         raise ValueError("%s: the last dimension must be contiguous" % what)
-    return t.data_ptr(), step if n > 1 else c
+    return t.data_ptr(), step if rows > 1 else cols
 
 
 def _vector(t, dtype, what, numel):
@@ -119,14 +117,14 @@ def zero_rms_norm(x, weight, eps, residual=None, h=None, y=None, q8=None, scale=
     Each output is written where a tensor is given; y, q8 * scale and h are [rows, cols], rstd [rows],
     scale [rows, ceil(cols / group)].  h may be residual or x in place, and so may y."""
     code, dt = _type(x, "x"), x.dtype
-    rows, cols = _sizes(x, "x")
-    px, ld_x = _matrix(x, dt, "x", rows, cols)
-    pr, ld_r = _matrix(residual, dt, "residual", rows, cols)
-    ph, ld_h = _matrix(h, dt, "h", rows, cols)
-    py, ld_y = _matrix(y, dt, "y", rows, cols)
+    size = rows, cols = _sizes(x, "x")
+    px, ld_x = _matrix(x, dt, "x", size)
+    pr, ld_r = _matrix(residual, dt, "residual", size)
+    ph, ld_h = _matrix(h, dt, "h", size)
+    py, ld_y = _matrix(y, dt, "y", size)
     pq, ld_q, ps = 0, cols, 0
     if q8 is not None:
-        pq, ld_q = _matrix(q8, torch.uint8 if q8.dtype is torch.uint8 else torch.float8_e4m3fn, "q8", rows, cols)
+        pq, ld_q = _matrix(q8, torch.uint8 if q8.dtype is torch.uint8 else torch.float8_e4m3fn, "q8", size)
     if scale is not None:
         ps = _vector(scale, _F32, "scale", rows * (-(-cols // group) if group > 0 else 1))
     args = RMS_NORM_ARGS.pack(code, group, rows, cols, eps, px, ld_x, pr, ld_r, _vector(weight, dt, "weight", cols), ph, ld_h,
@@ -149,11 +147,11 @@ def zero_rms_norm_backward(dy, h, weight, rstd, dx, dweight, workspace=None, dh=
     gradient dh that reaches h from elsewhere.  workspace: a float32 tensor of at least
     zero_rms_norm_workspace(rows, cols) elements."""
     code, dt = _type(h, "h"), h.dtype
-    rows, cols = _sizes(h, "h")
-    ph, ld_h = _matrix(h, dt, "h", rows, cols)
-    pdy, ld_dy = _matrix(dy, dt, "dy", rows, cols)
-    pdh, ld_dh = _matrix(dh, dt, "dh", rows, cols)
-    pdx, ld_dx = _matrix(dx, dt, "dx", rows, cols)
+    size = rows, cols = _sizes(h, "h")
+    ph, ld_h = _matrix(h, dt, "h", size)
+    pdy, ld_dy = _matrix(dy, dt, "dy", size)
+    pdh, ld_dh = _matrix(dh, dt, "dh", size)
+    pdx, ld_dx = _matrix(dx, dt, "dx", size)
     pw, n = _room(workspace, _F32, "workspace")
     args = RMS_NORM_BACKWARD_ARGS.pack(code, 0, rows, cols, pdy, ld_dy, ph, ld_h, _vector(weight, dt, "weight", cols),
                                _vector(rstd, _F32, "rstd", rows), pdh, ld_dh, pdx, ld_dx,
@@ -176,8 +174,8 @@ def zero_route(logits, index, weight, score="softmax", bias=None, groups=1, top_
     [tokens, k], in falling order of the keys.  score: "softmax" or "sigmoid"; bias [experts] float32 acts on the
     choice alone; groups > 1 keeps the top_groups groups of the largest sums of their group_top largest keys."""
     code = _type(logits, "logits")
-    rows, experts = _sizes(logits, "logits")
-    pl, ld = _matrix(logits, logits.dtype, "logits", rows, experts)
+    size = rows, experts = _sizes(logits, "logits")
+    pl, ld = _matrix(logits, logits.dtype, "logits", size)
     k = index.shape[-1]
     args = ROUTE_ARGS.pack(code, _score(score), rows, experts, k, groups, top_groups, group_top, bool(renormalise), scale,
                      pl, ld, _vector(bias, _F32, "bias", experts), _vector(index, _I32, "index", rows * k),
@@ -212,9 +210,9 @@ def zero_route_backward(logits, index, dweight, dlogits, score="softmax", bias=N
     """The gradient of zero_route's logits into dlogits [tokens, experts] (may be logits in place) from that of its
     weights, dweight [tokens, k] float32, and its index."""
     code, dt = _type(logits, "logits"), logits.dtype
-    rows, experts = _sizes(logits, "logits")
-    pl, ld = _matrix(logits, dt, "logits", rows, experts)
-    pd, ld_d = _matrix(dlogits, dt, "dlogits", rows, experts)
+    size = rows, experts = _sizes(logits, "logits")
+    pl, ld = _matrix(logits, dt, "logits", size)
+    pd, ld_d = _matrix(dlogits, dt, "dlogits", size)
     k = index.shape[-1]
     args = ROUTE_BACKWARD_ARGS.pack(code, _score(score), rows, experts, k, bool(renormalise), 0, scale, pl, ld,
                              _vector(bias, _F32, "bias", experts), _vector(index, _I32, "index", rows * k),
@@ -227,9 +225,9 @@ def zero_route_backward(logits, index, dweight, dlogits, score="softmax", bias=N
 def _distill(fn, logits, teacher_index, teacher_logits, loss, stats, dlogits, dloss, labels, soft, hard, temperature,
              row_weight, grad_scale, stream):
     code, dt = _type(logits, "logits"), logits.dtype
-    rows, vocab = _sizes(logits, "logits")
-    pl, ld = _matrix(logits, dt, "logits", rows, vocab)
-    pd, ld_d = _matrix(dlogits, dt, "dlogits", rows, vocab)
+    size = rows, vocab = _sizes(logits, "logits")
+    pl, ld = _matrix(logits, dt, "logits", size)
+    pd, ld_d = _matrix(dlogits, dt, "dlogits", size)
     k, teacher, pi, pt = 0, ZERO_F32, 0, 0
     if teacher_index is not None:
         k = teacher_index.shape[-1]
