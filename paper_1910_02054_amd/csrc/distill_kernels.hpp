@@ -229,7 +229,9 @@ __device__ __forceinline__ void distill_row(const zero_distill_args_t& a, const 
 
     // the row's maximum and sums, of this thread, then of its wave
     float m = edge, s = 0.f, s1 = 0.f;
-    if constexpr (kInRegisters) {
+    if constexpr (MODE == kDistillBack) {
+        // both are in the statistics
+    } else if constexpr (kInRegisters) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             m = max_of<T>(v[i], m);
@@ -241,7 +243,7 @@ __device__ __forceinline__ void distill_row(const zero_distill_args_t& a, const 
             keep_packed(v[i]);
             add_terms<T, KIND>(v[i], x, x1, s, s1);
         }
-    } else if constexpr (MODE != kDistillBack) {
+    } else {
         {
             m = edge == edge ? edge : -inf;
             const Against<T> x(k.c, m), x1(k.c1, m);

@@ -319,12 +319,6 @@ int with_distill_shape(int64_t vectors, F f) {
     return f(DistillShape<1024, 0>{});
 }
 
-template <typename F>
-int with_stream_shape(int64_t vectors, F f) {
-    if (vectors <= 1024) return f(DistillShape<256, 0>{});
-    return f(DistillShape<1024, 0>{});
-}
-
 template <int MODE>
 int distill(const char* fn, const zero_distill_args_t* args, void* stream_) {
     if (!args)
@@ -390,10 +384,7 @@ int distill(const char* fn, const zero_distill_args_t* args, void* stream_) {
             HIP_TRY(hipGetLastError());
             return ZERO_OK;
         };
-        if constexpr (MODE != zo::kDistillBack)
-            return with_distill_shape(vectors, launch);
-        else
-            return with_stream_shape(vectors, launch);
+        return with_distill_shape(vectors, launch);
     });
 }
 
