@@ -49,7 +49,8 @@ __device__ __forceinline__ void load_keys(const typename T::elem* p, int col, in
     }
 }
 
-// The two largest of a run of lanes (a power of two up to 64, the same in the whole grid).
+// The two largest of a run of lanes (a power of two up to 32, the same in the whole grid: with two groups
+// or more a group has half a wave at most).
 struct Top2 {
     uint32_t a, b;
 };
@@ -64,12 +65,9 @@ __device__ __forceinline__ Top2 top2_dpp(Top2 t) {
     return top2(t.a, t.b, dpp<CTRL>(t.a), dpp<CTRL>(t.b));
 }
 
-template <bool HALF>
 __device__ __forceinline__ Top2 top2_swap(Top2 t) {
-    const auto a = HALF ? __builtin_amdgcn_permlane32_swap(t.a, t.a, false, false)
-                        : __builtin_amdgcn_permlane16_swap(t.a, t.a, false, false);
-    const auto b = HALF ? __builtin_amdgcn_permlane32_swap(t.b, t.b, false, false)
-                        : __builtin_amdgcn_permlane16_swap(t.b, t.b, false, false);
+    const auto a = __builtin_amdgcn_permlane16_swap(t.a, t.a, false, false);
+    const auto b = __builtin_amdgcn_permlane16_swap(t.b, t.b, false, false);
     return top2(a[0], b[0], a[1], b[1]);
 }
 
@@ -83,9 +81,7 @@ __device__ __forceinline__ Top2 run_top2(Top2 t, int lanes) {
     if (lanes >= 16)
         t = top2_dpp<0x140>(t);
     if (lanes >= 32)
-        t = top2_swap<false>(t);
-    if (lanes >= 64)
-        t = top2_swap<true>(t);
+        t = top2_swap(t);
     return t;
 }
 

@@ -13,7 +13,6 @@
 
 namespace zo {
 
-using zs::f32x4;
 using zs::u32x2;
 using zs::u32x4;
 
@@ -117,10 +116,10 @@ __device__ __forceinline__ void store_vec(typename T::elem* p, u32x4 v) {
 
 // The 16 bytes of row `p` from column `col`, elements at or past `cols` filled from
 // `fill` (a word of two or one of them).
-template <typename T, bool NT = false>
+template <typename T>
 __device__ __forceinline__ u32x4 load_row(const typename T::elem* p, int col, int cols, uint32_t fill) {
     if (col + T::kPer <= cols)
-        return load_vec<T, NT>(p + col);
+        return load_vec<T, false>(p + col);
     u32x4 v = {fill, fill, fill, fill};
     if constexpr (T::kPer == 4) {
 #pragma unroll
@@ -142,10 +141,10 @@ __device__ __forceinline__ u32x4 load_row(const typename T::elem* p, int col, in
 }
 
 // Stores the 16 bytes at column `col` of row `p`, but for elements at or past `cols`.
-template <typename T, bool NT = false>
+template <typename T>
 __device__ __forceinline__ void store_row(typename T::elem* p, int col, int cols, u32x4 v) {
     if (col + T::kPer <= cols) {
-        store_vec<T, NT>(p + col, v);
+        store_vec<T, false>(p + col, v);
         return;
     }
     if constexpr (T::kPer == 4) {
