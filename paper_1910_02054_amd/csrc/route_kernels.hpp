@@ -240,15 +240,31 @@ __global__ __launch_bounds__(kOrderBlock) void k_route_order(const int32_t* inde
     const int64_t part = run / kOrderWaves;  // a wave's slots: neighbours, in the order of the waves
     const int64_t from = blockIdx.x * run + wave * part;
     const int64_t end = from + part < slots ? from + part : slots;
-    for (int e = threadIdx.x; e < kOrderWaves * keys; e += kOrderBlock)
-        place[e / keys][e % keys] = 0;
-    __syncthreads();
-    constexpr int kBatch = 4;  // keys under way at a time
-    for (int64_t s0 = from + lane; s0 < end; s0 += 64 * kBatch) {
-        int key[kBatch];
+    constexpr int kBatch = 4;  // keys under way at a time; a wave's first batch stays in its registers
+    auto load_keys = [&](int* key, int64_t s0) {
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i)
-            key[i] = s0 + 64 * i < end ? slot_key(index, s0 + 64 * i, experts) : -1;
+        for (int i = 0; i < kBatch; ++i) {
+            const int64_t s = s0 + 64 * i + lane;
+            key[i] = s < end ? slot_key(index, s, experts) : -1;
+        }
+    };
+    int first[kBatch];
+    load_keys(first, from);
+
+    for (int e = threadIdx.x; e < keys; e += kOrderBlock)
+#pragma unroll
+        for (int w = 0; w < kOrderWaves; ++w)
+            place[w][e] = 0;
+    __syncthreads();
+    for (int64_t s0 = from; s0 < end; s0 += 64 * kBatch) {
+        int key[kBatch];
+        if (s0 == from) {
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                key[i] = first[i];
+        } else {
+            load_keys(key, s0);
+        }
 #pragma unroll
         for (int i = 0; i < kBatch; ++i)
             if (key[i] >= 0)
@@ -257,24 +273,44 @@ __global__ __launch_bounds__(kOrderBlock) void k_route_order(const int32_t* inde
     __syncthreads();
 
     // this thread's keys: all slots of each, and those of the workgroups before this one
-    int32_t all[OWN], prior[OWN], mine = 0;
+    int32_t all[OWN], prior[OWN];
 #pragma unroll
     for (int j = 0; j < OWN; ++j) {
         const int e = threadIdx.x * OWN + j;
         all[j] = prior[j] = 0;
-        if (e < keys) {
-            if (counts) {
-#pragma unroll 16
-                for (unsigned b = 0; b < gridDim.x; ++b) {
-                    const int32_t c = counts[(int64_t)b * keys + e];
-                    all[j] += c;
-                    prior[j] += b < blockIdx.x ? c : 0;
-                }
-            } else {
+        if (counts && e < keys) {
+            // sixteen loads under way; the last batch reads the last run again where there are none
+            const int runs = (int)gridDim.x, before = (int)blockIdx.x;
+            const int32_t* p = counts + e;
+            for (int b0 = 0; b0 < runs; b0 += 16, p += 16 * keys) {
+                int32_t c[16];
+                if (b0 + 16 <= runs) {
 #pragma unroll
-                for (int w = 0; w < kOrderWaves; ++w)
-                    all[j] += place[w][e];
+                    for (int i = 0; i < 16; ++i)
+                        c[i] = p[i * keys];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        c[i] = p[(b0 + i < runs ? i : runs - 1 - b0) * keys];
+                        c[i] = b0 + i < runs ? c[i] : 0;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    all[j] += c[i];
+                    prior[j] += b0 + i < before ? c[i] : 0;
+                }
             }
+        }
+    }
+    int32_t mine = 0;
+#pragma unroll
+    for (int j = 0; j < OWN; ++j) {
+        const int e = threadIdx.x * OWN + j;
+        if (!counts && e < keys) {
+#pragma unroll
+            for (int w = 0; w < kOrderWaves; ++w)
+                all[j] += place[w][e];
         }
         mine += all[j];
     }
@@ -311,10 +347,12 @@ __global__ __launch_bounds__(kOrderBlock) void k_route_order(const int32_t* inde
     const int bits = 32 - __builtin_clz(keys);
     for (int64_t s0 = from; s0 < end; s0 += 64 * kBatch) {
         int key[kBatch];
+        if (s0 == from) {
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            const int64_t s = s0 + 64 * i + lane;
-            key[i] = s < end ? slot_key(index, s, experts) : -1;
+            for (int i = 0; i < kBatch; ++i)
+                key[i] = first[i];
+        } else {
+            load_keys(key, s0);
         }
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {

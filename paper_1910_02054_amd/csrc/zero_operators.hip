@@ -257,18 +257,16 @@ int token_lanes(int experts, int k, int groups) {
     return lanes;
 }
 
-// Slots that a workgroup of the ordering aims at: with few, more workgroups (24594 slots of 60 experts: 9.5
-// us with 1024, 10.9 with 2048); with many, fewer counts that each has to read (131072 of 256: 11.4 and 10.2).
-constexpr int64_t kOrderMaxBlocks = 256;
-
-int64_t order_run(int64_t slots) { return slots < 65536 && slots > 2048 ? 1024 : 2048; }
+// Slots that a workgroup of the ordering aims at: with fewer, every workgroup has more counts to read (131072
+// slots of 256 experts: 10.0 us, 11.5 with 1024; 24594 of 60: 7.6 and 7.5).
+constexpr int64_t kOrderRun = 2048, kOrderMaxBlocks = 256;
 
 struct OrderPlan {
     int64_t blocks, run;
 };
 
 OrderPlan order_plan(int64_t slots) {
-    int64_t blocks = std::max<int64_t>(1, std::min(kOrderMaxBlocks, div_up(slots, order_run(slots))));
+    int64_t blocks = std::max<int64_t>(1, std::min(kOrderMaxBlocks, div_up(slots, kOrderRun)));
     const int64_t run = std::max<int64_t>(1, div_up(div_up(slots, blocks), zo::kOrderBlock)) * zo::kOrderBlock;
     blocks = std::max<int64_t>(1, div_up(slots, run));
     return OrderPlan{blocks, run};
