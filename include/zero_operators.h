@@ -237,7 +237,7 @@ typedef struct {
     int32_t teacher_dtype; /* of teacher_logits                                     */
     int64_t rows, vocab;   /* vocab in [1, 2^30]                                    */
     int32_t k, pad_;       /* entries a row, 0 <= k <= ZERO_DISTILL_MAX_K           */
-    double temperature;    /* > 0, finite                                           */
+    double temperature;    /* in [1e-30, 1e30]                                      */
     double soft, hard;     /* finite                                                */
     double grad_scale;     /* finite; the loss scale                                */
     const void* logits;    /* [rows, vocab]                                         */

@@ -14,6 +14,10 @@
 // hold a listed token aside in LDS and writing each value once takes longer: a look at a mark for
 // every vector costs more than the few lines that are written twice; 4096 rows of 50304
 // f16 with 64 entries 155 us in place of 144.)
+//
+// Bound by HBM: 4096 rows of 50257 f16, 64 entries, both terms, 143 us, 5.8 TB/s (a second exponential an element, for
+// temperatures other than 1 and 2 with a hard term, 154); 1024 of 131072 bf16 107 us, 5.0: such a row leaves
+// one workgroup a compute unit; 65536 of 2048 f16 111 us, 5.1; the loss alone of 4096 of 50257 70 us, 5.9.
 #pragma once
 
 #include "row_ops.hpp"
@@ -89,7 +93,9 @@ struct Against {
 
 constexpr int kBatch = 4;  // vectors at a time of a row that is read as it is needed
 
-// Whether a row goes past the caches.
+// Whether a row goes past the caches: long ones, which do not come back (4096 of 50304 f16 144 us in place of 155); the
+// tokens' values, written after the rest of a row, find short rows' lines still in L2 (16384 of 8192: 110 us, 137 to
+// 178 past it).
 constexpr bool past_caches(int threads) { return threads >= 1024; }
 
 // How the soft and the hard term share the exponentials of an element.

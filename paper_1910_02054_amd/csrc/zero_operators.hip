@@ -332,8 +332,8 @@ int distill(const char* fn, const zero_distill_args_t* args, void* stream_) {
         return fail(ZERO_EINVAL, "%s: vocab = %lld is outside [1, 2^30]", fn, (long long)a.vocab);
     if (a.k < 0 || a.k > ZERO_DISTILL_MAX_K)
         return fail(ZERO_EINVAL, "%s: k = %d is outside [0, %d]", fn, a.k, ZERO_DISTILL_MAX_K);
-    if (!is_fin(a.temperature) || !(a.temperature > 0.0))
-        return fail(ZERO_EINVAL, "%s: temperature must be finite and > 0", fn);
+    if (!(a.temperature >= 1e-30 && a.temperature <= 1e30))  // its reciprocal is held in fp32
+        return fail(ZERO_EINVAL, "%s: temperature must lie in [1e-30, 1e30]", fn);
     if (!is_fin(a.soft) || !is_fin(a.hard) || !is_fin(a.grad_scale))
         return fail(ZERO_EINVAL, "%s: soft, hard and grad_scale must be finite", fn);
     const bool back = MODE == zo::kDistillBack;

@@ -51,9 +51,9 @@ def _on(stream):
 
 
 def _type(t, what):
-    code = _TYPE.get(t.dtype)
+    code = _TYPE.get(getattr(t, "dtype", None))
     if code is None:
-        raise TypeError("%s: dtype %s not in %s" % (what, t.dtype, tuple(_TYPE)))
+        raise TypeError("%s must be a tensor of one of %s" % (what, tuple(_TYPE)))
     return code
 
 

@@ -546,6 +546,14 @@ def test_distill_masks(zo, dtype, vocab):
     assert math.isnan(loss[1].item()) and loss[9].item() == 0
 
 
+@pytest.mark.parametrize("dtype", C.TYPES)
+@pytest.mark.parametrize("tau", (1e-6, 1e-3, 50.0))
+def test_distill_temperatures(zo, dtype, tau):
+    """Far from 1 on both sides: a softmax that takes the largest alone, and an even one."""
+    for vocab in (700, 9000):
+        check_distill(zo, *distill_inputs(4, vocab, 10, dtype, dtype, 63), hard=0.25, tau=tau)
+
+
 def test_distill_overflow_reaches_the_shard_step(zo):
     """A loss scale that takes the gradient past binary16 gives inf, on which the shard step skips."""
     from paper_1910_02054_amd import binding as zb

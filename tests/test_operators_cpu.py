@@ -135,7 +135,8 @@ BAD = [
 ] + [
     (f, c) for f in ("zero_distill_step", "zero_distill_loss", "zero_distill_backward") for c in (
         dict(dtype=3), dict(teacher_dtype=4), dict(rows=-1), dict(vocab=0), dict(vocab=(1 << 30) + 1), dict(k=-1),
-        dict(k=1025), dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=NAN), dict(temperature=INF),
+        dict(k=1025), dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=NAN), dict(temperature=INF), dict(temperature=1e-31),
+        dict(temperature=1e31),
         dict(soft=NAN), dict(hard=INF), dict(grad_scale=NAN), dict(logits=0), dict(teacher_index=0),
         dict(teacher_logits=0), dict(ld_logits=999), dict(logits=A[0] + 1), dict(labels=A[3] + 2))
 ] + [
