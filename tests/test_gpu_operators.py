@@ -594,6 +594,41 @@ def test_distill_gradient_against_differences(zo):
             assert abs(float((both[0] - both[1]) / (2 * step)) - g[r, c].item()) < 2e-3
 
 
+# --- what only a device can refuse ---------------------------------------------------
+
+def test_arrays_outside_their_allocations_are_refused(zo):
+    """A size that overruns an array's allocation and memory that the device cannot reach are refused before a launch."""
+    x = torch.zeros(4, 256, dtype=F16, device="cuda")
+    w, y = torch.ones(256, dtype=F16, device="cuda"), torch.zeros_like(x)
+    host = torch.zeros(4, 256, dtype=F16)
+
+    def call(rows, px, py):
+        return zo._lib.zero_rms_norm(zo.RMS_NORM_ARGS.pack(1, 0, rows, 256, 1e-6, px, 256, 0, 256, w.data_ptr(), 0, 256, py,
+                                                          256, 0, 256, 0, 0), zo._on(None))
+
+    assert call(4, x.data_ptr(), y.data_ptr()) == 0
+    # more rows than the device has memory for (torch's own allocations may be longer than a tensor)
+    assert call(1 << 30, x.data_ptr(), x.data_ptr()) == -1
+    said = zo._lib.zero_last_error().decode()
+    assert "overruns its allocation" in said or "weight and y overlap" in said, said  # weight may lie in the span
+    assert call(4, host.data_ptr(), y.data_ptr()) == -1
+    assert "GPU-accessible" in zo._lib.zero_last_error().decode()
+    with pytest.raises(zo.ZeroError) as e:
+        zo.zero_rms_norm(x, w, -1.0, y=y)
+    assert e.value.code == -1 and "eps" in str(e.value)
+    with pytest.raises(ValueError):
+        zo.zero_rms_norm(x, w, 1e-6, y=torch.zeros(4, 255, dtype=F16, device="cuda"))
+    with pytest.raises(ValueError):
+        zo.zero_rms_norm(x.t().contiguous().t(), w, 1e-6, y=y)
+    with pytest.raises(TypeError):
+        zo.zero_rms_norm(x, w.float(), 1e-6, y=y)
+    with pytest.raises(TypeError):
+        zo.zero_rms_norm(x, w, 1e-6, y=host)
+    with pytest.raises(zo.ZeroError):  # rows that overlap the next ones
+        zo.zero_rms_norm(torch.as_strided(x, (3, 256), (100, 1)), w, 1e-6, y=torch.zeros(3, 256, dtype=F16, device="cuda"))
+    torch.cuda.synchronize()
+
+
 # --- streams, graphs, sizes ---------------------------------------------------------
 
 def all_calls(zo, seed, stream=None):
