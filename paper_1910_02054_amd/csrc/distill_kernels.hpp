@@ -93,10 +93,10 @@ struct Against {
 
 constexpr int kBatch = 4;  // vectors at a time of a row that is read as it is needed
 
-// Whether a row goes past the caches: long ones, which do not come back (4096 of 50304 f16 144 us in place of 155); the
-// tokens' values, written after the rest of a row, find short rows' lines still in L2 (16384 of 8192: 110 us, 137 to
-// 178 past it).
-constexpr bool past_caches(int threads) { return threads >= 1024; }
+// Whether a row goes past the caches: long ones, which do not come back (4096 of 50304 f16 144 us in place of 155, of
+// 32000 103 in place of 113); the tokens' values, written after the rest of a row, find short rows' lines still
+// in L2 (16384 of 8192: 111 us, 137 to 178 past it).
+constexpr bool past_caches(int threads, int vectors) { return vectors == 0 || threads * vectors > 1024; }
 
 // How the soft and the hard term share the exponentials of an element.
 enum DistillKind {
@@ -170,7 +170,7 @@ __device__ __forceinline__ void distill_row(const zero_distill_args_t& a, const 
     using elem = typename T::elem;
     constexpr int kPer = T::kPer, kWaves = NT / 64;
     constexpr bool kInRegisters = NV > 0;
-    constexpr bool kPast = past_caches(NT);
+    constexpr bool kPast = past_caches(NT, NV);
     static_assert(NT >= kMaxEdges, "a thread for each edge element");
     const int t = threadIdx.x, wave = t / 64, lane = t & 63, vocab = (int)a.vocab, entries = a.k;
     const float inf = __builtin_inff();
@@ -447,7 +447,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT < 1024 ||
             typename T::elem* dz = static_cast<typename T::elem*>(a.dlogits) + row * a.ld_dlogits;
             const Cut<T> cut(dz, (int)a.vocab);
             for (int n = threadIdx.x; n < cut.vectors; n += NT)
-                store_vec<T, past_caches(NT)>(dz + cut.head + n * T::kPer, u32x4{0, 0, 0, 0});
+                store_vec<T, past_caches(NT, NV)>(dz + cut.head + n * T::kPer, u32x4{0, 0, 0, 0});
             if ((int)threadIdx.x < cut.edges)
                 dz[cut.edge_column(threadIdx.x)] = T::of_f32(0.f);
         }
