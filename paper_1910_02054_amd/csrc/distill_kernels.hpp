@@ -94,7 +94,7 @@ struct Against {
 constexpr int kBatch = 4;  // vectors at a time of a row that is read as it is needed
 
 // Whether a row goes past the caches: long ones, which do not come back (4096 of 50304 f16 144 us in place of 155, of
-// 32000 103 in place of 113); the tokens' values, written after the rest of a row, find short rows' lines still
+// 32000 101 in place of 113); the tokens' values, written after the rest of a row, find short rows' lines still
 // in L2 (16384 of 8192: 111 us, 137 to 178 past it).
 constexpr bool past_caches(int threads, int vectors) { return vectors == 0 || threads * vectors > 1024; }
 
@@ -430,8 +430,11 @@ __device__ __forceinline__ void distill_row(const zero_distill_args_t& a, const 
 
 }
 
+// Waves a SIMD: all eight while the packed row leaves room in 64 registers, six of short workgroups with eight vectors
+// a thread (at eight they spill: 8192 rows of 11093 bf16 82 us in place of 80), and one workgroup of 1024 a
+// compute unit above that.
 template <typename T, int NT, int NV, int MODE>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NT < 1024 || NV <= 7 ? 8 : 4))) void k_distill(
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NV <= 7 ? 8 : NT < 1024 ? 6 : 4))) void k_distill(
     const zero_distill_args_t a, const DistillScalars k, int heads, int64_t first) {
     __shared__ DistillLds<NT> lds;
     const int64_t row = first + blockIdx.x;

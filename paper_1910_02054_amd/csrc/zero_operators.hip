@@ -299,7 +299,7 @@ int check_choice(const char* fn, int dtype, int score, int64_t rows, int experts
 // ---------------------------------------------------------------------------
 // Distillation.  Threads of a row's workgroup and vectors a thread: in registers while a
 // thread of 1024 needs at most 16, re-read above that (NV = 0).  Short rows take few threads with many
-// vectors each, so that more rows are under way on a compute unit: 8192 rows of 11093 bf16 82 us with
+// vectors each, so that more rows are under way on a compute unit: 8192 rows of 11093 bf16 80 us with
 // 256 threads of 8 vectors, 116 with 1024 of 2 (the loss alone 40 and 77); 65536 of 2048 f16 111 us with 128 of 2,
 // 164 with 256 of 1.
 // ---------------------------------------------------------------------------
