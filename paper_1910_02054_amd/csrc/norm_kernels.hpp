@@ -48,6 +48,25 @@ __device__ __forceinline__ void store_e4m3(uint8_t* p, const float* f) {
         *reinterpret_cast<u32_b*>(p) = pack_e4m3(f);
 }
 
+// y / scale, rounded once, for many y of one scale t: the product with the rounded reciprocal is off by up
+// to two roundings, which puts a quotient beside a midpoint of two codes (bf16 rows have many on one) on the other
+// side; the exact remainder of that product corrects it to the nearest fp32.  The remainder has
+// bits down to 2^-34 t ulp(1) where the code is not 0, so scales below 1 (least: 2^-100 / 448) are raised by 2^24 with their y.
+// An infinite scale leaves 0 of what is finite, and of -0 stays -0.
+struct Quotient {
+    float k, t, inv;
+    __device__ __forceinline__ explicit Quotient(float scale) : k(scale < 1.f ? 0x1p24f : 1.f) {
+        const bool inf = scale == __builtin_inff();
+        t = inf ? 0.f : scale * k;
+        inv = inf ? 0.f : 1.0f / t;
+    }
+    __device__ __forceinline__ float operator()(float y) const {
+        y *= k;
+        const float q = y * inv, excess = __builtin_fmaf(q, t, -y);
+        return __builtin_fmaf(-excess, inv, q);
+    }
+};
+
 // Largest over runs of `lanes` neighbouring lanes (a power of two, 4 to 64, the same in the whole grid).
 __device__ __forceinline__ uint32_t run_max(uint32_t x, int lanes) {
     const MaxU op;
@@ -231,16 +250,16 @@ __global__ __launch_bounds__(norm_block(LPR)) void k_rms_norm(const zero_rms_nor
         if (c < cols && (group ? (c & (group - 1)) == 0 : c == 0))
             scale[group ? c / group : 0] = t;
         if (held.has(i)) {
-            const float inv = 1.0f / t;
+            const Quotient over(t);
             float g[kPer];
 #pragma unroll
             for (int j = 0; j < kPer; ++j)
-                g[j] = f[i][j] * inv;
+                g[j] = over(f[i][j]);
             store_e4m3<kPer>(q + c, g);
         }
         if (i == held.slot) {
             held.odd([&](int j, int at) {
-                float g[4] = {fo[j] * (1.0f / t)};
+                float g[4] = {Quotient(t)(fo[j])};
                 q[at] = (uint8_t)pack_e4m3(g);
             });
         }

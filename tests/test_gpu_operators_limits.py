@@ -1,0 +1,71 @@
+"""The training operators on the GPU at the ends of their types' ranges, and at every shape of their kernels that the
+sizes of test_gpu_operators.py do not reach."""
+import math
+import os
+import sys
+
+import pytest
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+import operator_checks as C  # noqa: E402
+import test_gpu_operators as G  # noqa: E402
+from test_gpu_operators import Out, put  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def zo():
+    from paper_1910_02054_amd import operators
+    assert torch.cuda.is_available()
+    return operators
+
+
+# --- e4m3 codes -------------------------------------------------------------------
+
+def run_e4m3(zo, h, w, group, eps):
+    """(codes, scale, rstd) of the rows h, on the CPU."""
+    rows, cols = h.shape
+    q = Out(rows, cols, torch.uint8)
+    scale, rstd = Out(rows, -(-cols // group) if group else 1, F32), Out(rows, 1, F32)
+    zo.zero_rms_norm(put(h), w.cuda(), eps, q8=q.view, scale=scale.view, group=group, rstd=rstd.view)
+    torch.cuda.synchronize()
+    assert q.guards_intact() and scale.guards_intact() and rstd.guards_intact()
+    return q.view.cpu(), scale.view.cpu(), rstd.view.cpu()
+
+
+def e4m3(q):
+    return q.clamp(-448.0, 448.0).to(torch.float8_e4m3fn).view(torch.uint8)
+
+
+@pytest.mark.parametrize("dtype", C.TYPES)
+@pytest.mark.parametrize("rows,cols,group", ((5, 100, 0), (300, 1603, 64), (257, 4096, 128), (9, 8200, 0)))
+def test_codes_are_of_the_quotient(zo, rows, cols, group, dtype):
+    """y's fp32 value is two products of the row, the rstd that the call returned and the weight, and the scale is
+    returned too, so the code of fl(y / scale) has no room: not where 8-bit mantissas make the quotient a tie
+    either."""
+    g = C.rng(83, rows, cols)
+    h, w = C.normal(g, rows, cols).to(dtype), (1 + 0.1 * C.normal(g, cols)).to(dtype)
+    q, scale, rstd = run_e4m3(zo, h, w, group, 1e-6)
+    y = h.float() * rstd * w.float()
+    assert torch.equal(scale, torch.stack([p.abs().amax(1) for p in y.split(group or cols, 1)], 1) / 448.0)
+    assert torch.equal(q, e4m3(y / C.spread(scale, cols, group)))
+
+
+@pytest.mark.parametrize("exponent", (-126, -110, -100, -81, -79, 0, 60, 126))
+def test_codes_beside_the_ties(zo, exponent):
+    """Rows of ones have rstd 1, so y is the weight: each midpoint of two neighbouring codes times the scale, and its
+    three neighbours on both sides, under 40 scales."""
+    g = C.rng(89, exponent + 200)
+    v = torch.arange(127, dtype=torch.uint8).view(torch.float8_e4m3fn).float()
+    ties = (v[1:] + v[:-1]) / 2
+    for _ in range(40):
+        top = (torch.rand(1, generator=g) + 1.0) * 2.0 ** exponent
+        t = top.clamp(min=2.0 ** -100) / 448.0
+        w = torch.cat([top] + [(ties * t).view(torch.int32).add(k).view(F32) for k in range(-3, 4)])
+        w = torch.where(w <= top, w, top) * torch.where(torch.rand(w.shape, generator=g) < 0.5, -1.0, 1.0)
+        q, scale, rstd = run_e4m3(zo, torch.ones(1, w.numel()), w, 0, 0.0)
+        assert rstd.item() == 1.0 and scale.item() == t.item()
+        assert torch.equal(q[0], e4m3(w / t))
