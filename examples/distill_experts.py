@@ -84,7 +84,8 @@ class Student:
         zo.zero_route(self.routed, self.index, self.weight, score="sigmoid", bias=self.bias)
         zo.zero_route_order(self.index, EXPERTS, self.offsets, self.order, self.order_room)
         self.ends = self.offsets.tolist()
-        self.slots = self.order.long()
+        # past the last expert's run are the slots that got no expert (a token whose logits are all NaN has none)
+        self.slots = self.order[:self.ends[EXPERTS]].long()
         self.token = self.slots // CHOSEN
         self.ordered = self.y1[self.token]
         self.inner, self.out = [], []
