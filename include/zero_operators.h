@@ -189,7 +189,8 @@ int zero_route_workspace(int64_t slots, int32_t experts, int64_t* ints);
  * d_i = scale * dweight_i and s the scores,
  *   softmax:                  dlogit_e = s_e * (d_e - sum_j d_j s_j), d_e = 0 for the rest
  *   softmax, renormalised:    the same over the chosen ones, 0 for the rest
- *   sigmoid:                  dlogit_i = d_i s_i (1 - s_i), 0 for the rest
+ *   sigmoid:                  dlogit_i = d_i s_i (1 - s_i), 0 for the rest; 1 - s_i is taken from
+ *                             the logit, so saturated scores keep their slope
  *   sigmoid, renormalised:    d_i replaced by (d_i - sum_j d_j s_j / S) / S, S = sum_j s_j
  * Experts that are out get 0.  `index` holds no expert twice in a row. */
 typedef struct {

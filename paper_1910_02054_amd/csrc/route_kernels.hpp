@@ -427,13 +427,15 @@ __global__ __launch_bounds__(kRouteBlock) void k_route_back(const zero_route_bac
         mean = seg_reduce<LPT>(p * d, Add());
         g = whole ? p * d : p * (d - mean);
     } else {
-        const float s = has ? sigmoid(zi) : 0.f;
+        const float e = has ? expf(-zi) : 0.f, s = has ? 1.0f / (1.0f + e) : 0.f;
         float t = d;
         if (a.renormalise) {
             const float sum = fmaxf(seg_reduce<LPT>(s, Add()), 0x1p-126f);
             t = (d - seg_reduce<LPT>(d * s, Add()) / sum) / sum;
         }
-        g = t * s * (1.0f - s);
+        // 1 - s as e^-z s: from s, rounded beside 1, nothing of it is left from z = 17 on.  (Where e^-z is
+        // past fp32, s is 0.)
+        g = t * s * (fminf(e, 0x1.fffffep127f) * s);
     }
     __syncthreads();
     if (has)

@@ -69,3 +69,35 @@ def test_codes_beside_the_ties(zo, exponent):
         q, scale, rstd = run_e4m3(zo, torch.ones(1, w.numel()), w, 0, 0.0)
         assert rstd.item() == 1.0 and scale.item() == t.item()
         assert torch.equal(q[0], e4m3(w / t))
+
+
+# --- routing: saturated scores --------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", C.TYPES)
+@pytest.mark.parametrize("renorm", (False, True))
+def test_route_backward_of_saturated_scores(zo, renorm, dtype):
+    """The sigmoid's slope s (1 - s) where s is near 1: a few units of the slope itself, as an exponential, two sums and
+    two quotients leave, not of s."""
+    values = torch.tensor([-60.0, -40.0, -20.0, -16.0, -12.0, -5.0, 0.0, 5.0, 9.0, 12.0, 14.0, 16.0, 17.0, 18.0, 20.0,
+                           30.0, 40.0, 60.0, 80.0])
+    g = C.rng(97)
+    rows, experts, k = 64, 24, 6
+    z = values[torch.randint(0, len(values), (rows, experts), generator=g)].to(dtype)
+    index = torch.stack([torch.randperm(experts, generator=g)[:k] for _ in range(rows)])
+    dw = C.normal(g, rows, k).float()
+    zc, d = z.double().gather(1, index), dw.double() * 2.5
+    s, slope = torch.sigmoid(zc), torch.sigmoid(zc) * torch.sigmoid(-zc)
+    t, size = d, d.abs()
+    if renorm:
+        total = s.sum(1, keepdim=True)
+        t = (d - (d * s).sum(1, keepdim=True) / total) / total
+        size = (d.abs() + (d * s).abs().sum(1, keepdim=True) / total) / total
+    want = torch.zeros(rows, experts, dtype=torch.float64).scatter_add(1, index, t * slope)
+    units = 12 if not renorm else 60    # two sums of six terms, two quotients and a difference more
+    bound = torch.zeros_like(want).scatter_add(1, index, units * C.U * size * slope)
+    out = Out(rows, experts, dtype)
+    zo.zero_route_backward(put(z), index.int().cuda(), dw.cuda(), out.view, score="sigmoid", renormalise=renorm,
+                           scale=2.5)
+    torch.cuda.synchronize()
+    assert out.guards_intact()
+    C.within(out.view, want, C.rounded(bound, want, dtype), "dlogits")
