@@ -225,7 +225,9 @@ int zero_route_backward(const zero_route_backward_args_t* args, void* stream);
  *                         - hard * log q_1[label] )
  * The soft term is 0 in a row without entries (and where p_j = 0), the hard term in
  * one whose label lies outside [0, vocab); a row of weight 0 has loss 0 and is not
- * looked at.  A token listed twice counts twice.
+ * looked at.  A token listed twice counts twice.  The soft term is formed from differences
+ * of logits times soft * tau, so it is finite where its value is (a student masked by its
+ * type's lowest value included); its logarithms' rounding, 2^-20 or so, counts tau^2 times.
  * The gradient, with u = grad_scale * row_weight (* dloss where that is given):
  *   dlogits_v = u * ( soft * tau * (q_tau[v] - sum of p_j over entries of token v)
  *                     + hard * (q_1[v] - [v = label]) )

@@ -30,7 +30,8 @@ enum DistillMode { kDistillStep, kDistillLoss, kDistillBack };
 // What a call's rows share, computed on the host.
 struct DistillScalars {
     float c, c1;         // log2(e) / temperature, log2(e)
-    float soft_loss;     // soft * temperature^2 * ln 2: the loss of one bit of the sum
+    float bit;           // temperature * ln 2: one bit of a sum in units of the logits
+    float soft_in, soft_out;  // factors of soft * temperature: of an entry's term, where below 1, or of their sum
     float soft_grad;     // soft * temperature
     float hard;
     float scale;
@@ -61,16 +62,16 @@ __device__ __forceinline__ float any_f32(const void* p, int64_t i, int dtype) {
 //
 // The 16-bit types take one fused operation, c f - cm, where cm = c m is rounded once.  That
 // shifts every x of a row by the same amount (`shift`), which the quotients of terms and their sum
-// do not have; `log` takes it out.  The shift is small while cm is: from 2^20 on (logits
+// do not have; `log_sum` takes it out.  The shift is small while cm is: from 2^20 on (logits
 // no model has, but a row may hold nothing but the type's lowest value) neighbouring values
 // of the type lie at least 2^9 apart in x, so a term is 1 or 0 whatever the scale, and a
 // smaller c keeps cm at 2^20.  fp32 takes the difference first: its bytes leave the time for it.
 template <typename T>
 struct Against {
     static constexpr bool kFused = sizeof(typename T::elem) == 2;
-    float c, m, cm, whole;  // whole: c as given
+    float c, m, cm;
     __device__ __forceinline__ Against(float c_, float m_)
-        : c(c_), m(m_ == -__builtin_inff() ? 0.f : m_), cm(c * m), whole(c_) {
+        : c(c_), m(m_ == -__builtin_inff() ? 0.f : m_), cm(c * m) {
         if (kFused && fabsf(cm) >= 0x1p20f && fabsf(m) < __builtin_inff()) {
             c = 0x1p20f / fabsf(m);
             cm = c * m;
@@ -84,10 +85,9 @@ struct Against {
     __device__ __forceinline__ float moved(float sum, const Against& from) const {
         return sum == 0.f ? 0.f : sum * exp2_fast(kFused && c == from.c ? from.cm - cm : (from.m - m) * c);
     }
-    // log2 of the quotient of f's term and the sum of all.
-    __device__ __forceinline__ float log(float f, float sum) const {
-        const float shift = kFused ? (*this)(m) : 0.f;
-        return (f - m) * whole - (log2_fast(sum) - shift);
+    // log2 of the sum of all terms without the shift, that is against m itself.
+    __device__ __forceinline__ float log_sum(float sum) const {
+        return log2_fast(sum) - (kFused ? (*this)(m) : 0.f);
     }
 };
 
@@ -331,27 +331,32 @@ __device__ __forceinline__ void distill_row(const zero_distill_args_t& a, const 
     sum = seg_reduce<64>(sum, Add());
     const float over = has_soft ? 1.f / sum : 0.f;
 
+    // log p_j - log q_tau[token_j] = ((t_j - top) - (z_j - m) + tau ln 2 (log2 S - log2 sum)) / tau, so with tau^2 before
+    // it a term is a difference of logits (and a few bits of the sums) times tau: nothing in it leaves fp32 before
+    // the loss does, whatever the temperature and also where the student holds the type's lowest value.
     if constexpr (MODE != kDistillBack) {
         if (wave == 0) {
-            const float teacher_bits = log2_fast(sum);
-            float loss = 0.f;
+            const float bits = k.bit * (x.log_sum(s) - log2_fast(sum));
+            // temperature 1; kSquare's sum has twice the exponents of temperature 2, its shift too
+            const float shift = Against<T>::kFused && KIND == kSquare ? 2.f * x(m) - x1(m) : 0.f;
+            const float nats = 0.6931471805599453f * (x1.log_sum(s1) - shift);
+            float soft = 0.f, hard = 0.f;
             for (int j = lane; j < all; j += 64) {
                 if (token_of[j] < 0)
                     continue;
-                const float f = z_of[j];
+                const float below = x.m - z_of[j];
                 if (j == entries) {
-                    // temperature 1; kSquare's sum has twice the exponents of temperature 2, its shift too
-                    const float shift = Against<T>::kFused && KIND == kSquare ? 2.f * x(m) - x1(m) : 0.f;
-                    loss -= k.hard * 0.6931471805599453f * (x1.log(f, s1) + shift);
+                    hard = k.hard * (below + nats);
                 } else if (has_soft) {
-                    const float e = exponent_of(j), p = exp2_fast(e) * over;
+                    const float p = exp2_fast(exponent_of(j)) * over;
                     if (p != 0.f)
-                        loss += k.soft_loss * (p * ((e - teacher_bits) - x.log(f, s)));
+                        soft += p * (k.soft_in * ((teacher_of[j] - top) + below + bits));
                 }
             }
-            loss = seg_reduce<64>(loss, Add());
+            soft = seg_reduce<64>(soft, Add());
+            hard = seg_reduce<64>(hard, Add());
             if (lane == 0)
-                a.loss[row] = weight * loss;
+                a.loss[row] = weight * ((has_soft ? k.soft_out * soft : 0.f) + hard);
         }
     }
 

@@ -371,8 +371,10 @@ int distill(const char* fn, const zero_distill_args_t* args, void* stream_) {
     zo::DistillScalars k;
     k.c = (float)(log2e / (a.soft != 0.0 ? a.temperature : 1.0));  // the hard term alone is of temperature 1
     k.c1 = (float)log2e;
-    k.soft_loss = (float)(a.soft * a.temperature * a.temperature * ln2);
+    k.bit = (float)(a.temperature * ln2);
     k.soft_grad = (float)(a.soft * a.temperature);
+    k.soft_in = std::fabs(k.soft_grad) < 1.f ? k.soft_grad : 1.f;
+    k.soft_out = std::fabs(k.soft_grad) < 1.f ? 1.f : k.soft_grad;
     k.hard = a.labels ? (float)a.hard : 0.f;
     k.scale = (float)a.grad_scale;
     return with_type(a.dtype, [&](auto type) {

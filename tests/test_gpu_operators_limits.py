@@ -101,3 +101,77 @@ def test_route_backward_of_saturated_scores(zo, renorm, dtype):
     torch.cuda.synchronize()
     assert out.guards_intact()
     C.within(out.view, want, C.rounded(bound, want, dtype), "dlogits")
+
+
+# --- distillation: masks and temperatures ------------------------------------------------
+
+def run_loss(zo, z, index, teacher, labels=None, **kw):
+    """The losses [2, rows] by the step and by the call of their own."""
+    both = torch.empty(2, z.shape[0], device="cuda")
+    args = (put(z), None if index is None else index.cuda(), None if teacher is None else teacher.cuda())
+    kw["labels"] = None if labels is None else labels.cuda()
+    zo.zero_distill_step(*args, both[0], torch.empty(z.shape, dtype=z.dtype, device="cuda"), **kw)
+    zo.zero_distill_loss(*args, both[1], **kw)
+    return both.cpu()
+
+
+@pytest.mark.parametrize("dtype", C.TYPES)
+@pytest.mark.parametrize("vocab", (300, 5000, 140000))
+@pytest.mark.parametrize("tau", (1.0, 2.0, 1.5))
+def test_distill_wants_a_token_at_the_lowest_value(zo, tau, vocab, dtype):
+    """A student masked by its type's lowest value, not by -inf, where the teacher or the label wants the token: the loss is
+    the gap times the token's share, which fp32 holds.  Each loss is one product of the largest term, a few units."""
+    g = C.rng(101, vocab)
+    z = C.normal(g, 4, vocab)
+    index = torch.tensor([[3, 9, 20]] * 4, dtype=torch.int32)
+    teacher = torch.tensor([[1.0, 2.0, 0.5]] * 4)
+    labels = torch.tensor([5, 7, 50, 60], dtype=torch.int32)
+    low = torch.finfo(dtype).min
+    z[0, 9] = low            # the teacher's largest
+    z[1, 7] = low            # the label
+    z[2, :40] = low          # every token of the list
+    z = z.to(dtype)
+    soft, hard = 0.05, 0.25
+    loss = run_loss(zo, z, index, teacher, labels, soft=soft, hard=hard, temperature=tau)
+    want, _, _, _ = C.distill(z, index, teacher, labels, soft, hard, tau, None, 1.0)
+    assert torch.isfinite(want.float()).all()
+    C.within(loss, want.expand(2, -1), 60 * C.U * want.abs() + 60 * C.U * 20, "loss")
+
+
+@pytest.mark.parametrize("dtype", C.TYPES)
+@pytest.mark.parametrize("tau", (1e-30, 1e-25, 1e-22, 1e-19, 1e-12, 1e-6))
+def test_distill_low_temperatures(zo, tau, dtype):
+    """Next to nothing, the teacher's largest takes all, the student's too: the loss is soft tau times the gap between its
+    maximum and the logit of the teacher's token."""
+    g = C.rng(103)
+    for vocab in (700, 9000):
+        z, teacher = (C.normal(g, 5, vocab) * 4).to(dtype), C.normal(g, 5, 6)
+        index = torch.stack([torch.randperm(vocab, generator=g)[:6] for _ in range(5)]).int()
+        at = index.gather(1, teacher.float().argmax(1, keepdim=True)).long()
+        want = 0.7 * tau * (z.double().amax(1) - z.double().gather(1, at)[:, 0])
+        loss = run_loss(zo, z, index, teacher.float(), soft=0.7, temperature=tau)
+        # where the two agree, what the two sums' logarithms leave of tau^2
+        C.within(loss, want.expand(2, -1), 12 * C.U * want + 60 * C.U * tau ** 2 + C.TINY[F32], "loss")
+
+
+@pytest.mark.parametrize("dtype", C.TYPES)
+@pytest.mark.parametrize("tau", (1e3, 1e10, 1e18))
+def test_distill_high_temperatures(zo, tau, dtype):
+    """An even student against an even list of a part of the vocabulary: soft tau^2 ln(vocab / entries) in the main."""
+    g = C.rng(107)
+    z, teacher = C.normal(g, 5, 4000).to(dtype), C.normal(g, 5, 10).float()
+    index = torch.stack([torch.randperm(4000, generator=g)[:10] for _ in range(5)]).int()
+    want, _, _, _ = C.distill(z, index, teacher, None, 0.7, 0.0, tau, None, 1.0)
+    loss = run_loss(zo, z, index, teacher, soft=0.7, temperature=tau)
+    C.within(loss, want.expand(2, -1), 60 * C.U * want, "loss")
+
+
+@pytest.mark.parametrize("dtype", C.TYPES)
+@pytest.mark.parametrize("tau", (1e20, 1e30))
+def test_distill_whole_list_at_any_temperature(zo, tau, dtype):
+    """A list of the whole vocabulary, on which the student agrees with the teacher: nothing is left but rounding, of which
+    the header says that it grows with tau^2; but never a NaN."""
+    z = torch.tensor([[1.0, 2.0, 0.5, -1.0]] * 3).to(dtype)
+    index = torch.arange(4, dtype=torch.int32).repeat(3, 1)
+    loss = run_loss(zo, z, index, z.float(), temperature=tau)
+    assert not loss.isnan().any()
