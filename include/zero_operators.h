@@ -155,7 +155,7 @@ typedef struct {
     int32_t groups, top_groups, group_top; /* groups divides experts, at most 64; group_top = 2
                                               needs groups of two or more           */
     int32_t renormalise;
-    double scale;        /* finite                                                  */
+    double scale;        /* finite in fp32                                          */
     const void* logits;  /* [rows, experts]                                         */
     int64_t ld_logits;
     const float* bias;   /* [experts]; NULL: none                                   */
@@ -241,8 +241,8 @@ typedef struct {
     int64_t rows, vocab;   /* vocab in [1, 2^30]                                    */
     int32_t k, pad_;       /* entries a row, 0 <= k <= ZERO_DISTILL_MAX_K           */
     double temperature;    /* in [1e-30, 1e30]                                      */
-    double soft, hard;     /* finite                                                */
-    double grad_scale;     /* finite; the loss scale                                */
+    double soft, hard;     /* soft * temperature and hard finite in fp32            */
+    double grad_scale;     /* finite in fp32; the loss scale                        */
     const void* logits;    /* [rows, vocab]                                         */
     int64_t ld_logits;
     const int32_t* teacher_index;  /* [rows, k], close together; NULL if k = 0      */

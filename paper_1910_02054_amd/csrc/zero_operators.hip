@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 
@@ -45,6 +46,9 @@ struct Matrix {
 };
 
 size_t elem_size(int dtype) { return dtype == ZERO_F32 ? 4 : 2; }
+
+// Whether x is finite as the kernels have it.
+bool is_fin32(double x) { return std::fabs(x) <= FLT_MAX; }
 
 bool known_type(int dtype) { return dtype == ZERO_F32 || dtype == ZERO_F16 || dtype == ZERO_BF16; }
 
@@ -291,8 +295,8 @@ int check_choice(const char* fn, int dtype, int score, int64_t rows, int experts
                     experts);
     if (rows > INT32_MAX / k)
         return fail(ZERO_EINVAL, "%s: rows * k = %lld * %d is not below 2^31", fn, (long long)rows, k);
-    if (!is_fin(scale))
-        return fail(ZERO_EINVAL, "%s: scale must be finite", fn);
+    if (!is_fin32(scale))
+        return fail(ZERO_EINVAL, "%s: scale must be finite in fp32", fn);
     return ZERO_OK;
 }
 
@@ -337,8 +341,8 @@ int distill(const char* fn, const zero_distill_args_t* args, void* stream_) {
         return fail(ZERO_EINVAL, "%s: k = %d is outside [0, %d]", fn, a.k, ZERO_DISTILL_MAX_K);
     if (!(a.temperature >= 1e-30 && a.temperature <= 1e30))  // its reciprocal is held in fp32
         return fail(ZERO_EINVAL, "%s: temperature must lie in [1e-30, 1e30]", fn);
-    if (!is_fin(a.soft) || !is_fin(a.hard) || !is_fin(a.grad_scale))
-        return fail(ZERO_EINVAL, "%s: soft, hard and grad_scale must be finite", fn);
+    if (!is_fin32(a.soft * a.temperature) || !is_fin32(a.hard) || !is_fin32(a.grad_scale))
+        return fail(ZERO_EINVAL, "%s: soft * temperature, hard and grad_scale must be finite in fp32", fn);
     const bool back = MODE == zo::kDistillBack;
     if (back ? a.loss != nullptr : a.dloss != nullptr)
         return fail(ZERO_EINVAL, "%s: %s must be NULL", fn, back ? "loss" : "dloss");
