@@ -65,7 +65,8 @@ extern "C" {
  * scale = max(largest |y| of the group, 2^-100) / 448,  q8 = e4m3(y / scale).
  * e4m3 is the OCP 8-bit float with largest value 448 and no infinities; it is
  * rounded to nearest even.  A NaN in a row makes the row's rstd, y, q8 and scales
- * NaN. */
+ * NaN; an infinity makes rstd 0.  Finite rows have the rstd and y of the formula wherever fp32 holds
+ * that rstd, also where squares or eps would leave fp32's range. */
 typedef struct {
     int32_t dtype;       /* of x, residual, weight, h, y                            */
     int32_t group;       /* columns of one scale; 0: one scale a row                */

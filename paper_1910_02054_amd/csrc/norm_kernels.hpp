@@ -116,6 +116,19 @@ struct Held {
 // 16384 of 4096 95 in place of 108; rows of 512 lose by it (13.6, 12.7).
 constexpr bool norm_past(int lpr, int nv) { return lpr * nv > 64; }
 
+// The reciprocal root of a row whose sum of squares, or eps, has left fp32's range (or is so small that squares are lost): the
+// squares again, of elements scaled by 2^-80 or 2^80, and the rest in fp64.  A row that holds an infinity or a
+// NaN comes out as it went in.  `total` is the mean and eps in fp32, which tells such rows: where it lies in
+// [2^-85, inf) all that was lost is below 2^-49 of it.
+constexpr float kLeastTotal = 0x1p-85f;
+
+template <int LPR, typename F>
+__device__ __forceinline__ float far_rstd(float total, double eps, int cols, float* lds, F sum_of_squares) {
+    const float k = total < kLeastTotal ? 0x1p80f : 0x1p-80f;
+    const double sum = row_reduce<LPR>(sum_of_squares(k), lds, Add());
+    return (float)(1.0 / sqrt(sum / ((double)k * k * cols) + eps));
+}
+
 template <typename T, int LPR, int NV>
 __global__ __launch_bounds__(norm_block(LPR)) void k_rms_norm(const zero_rms_norm_args_t a, int64_t first) {
     // a run of lanes that shares a scale lies in one slot's lanes, or is all of them
@@ -124,6 +137,7 @@ __global__ __launch_bounds__(norm_block(LPR)) void k_rms_norm(const zero_rms_nor
     constexpr int kPer = T::kPer, kBlock = norm_block(LPR);
     constexpr bool PAST = norm_past(LPR, NV);
     __shared__ float sums[LPR > 64 ? LPR / 64 : 1];
+    __shared__ float far_sums[LPR > 64 ? LPR / 64 : 1];
     __shared__ uint32_t tops[LPR > 64 ? LPR / 64 : 1];
     const int lane = threadIdx.x % LPR, cols = (int)a.cols;
     const int64_t row = first + (int64_t)blockIdx.x * (kBlock / LPR) + threadIdx.x / LPR;
@@ -189,7 +203,19 @@ __global__ __launch_bounds__(norm_block(LPR)) void k_rms_norm(const zero_rms_nor
         sum = __builtin_fmaf(fo[j], fo[j], sum);
     });
     sum = row_reduce<LPR>(sum, sums, Add());
-    const float rstd = 1.0f / sqrtf(sum / (float)cols + (float)a.eps);
+    const float total = sum / (float)cols + (float)a.eps;
+    float rstd = 1.0f / sqrtf(total);
+    if (!(total >= kLeastTotal && total < __builtin_inff()))  // the same for all lanes of a row
+        rstd = far_rstd<LPR>(total, a.eps, cols, far_sums, [&](float k) {
+            float s = 0.f;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int j = 0; j < kPer; ++j)
+                    s = __builtin_fmaf(f[i][j] * k, f[i][j] * k, s);
+            held.odd([&](int j, int) { s = __builtin_fmaf(fo[j] * k, fo[j] * k, s); });
+            return s;
+        });
     if (a.rstd && lane == 0)
         a.rstd[row] = rstd;
 

@@ -175,3 +175,70 @@ def test_distill_whole_list_at_any_temperature(zo, tau, dtype):
     index = torch.arange(4, dtype=torch.int32).repeat(3, 1)
     loss = run_loss(zo, z, index, z.float(), temperature=tau)
     assert not loss.isnan().any()
+
+
+# --- norm: the ends of the range ----------------------------------------------------------
+
+WIDE = (3, 8, 64, 100, 200, 512, 1603, 4100, 8200, 20000, 32768)
+
+
+@pytest.mark.parametrize("dtype", (BF16, F32))
+@pytest.mark.parametrize("rows", (9, 300))
+@pytest.mark.parametrize("cols", WIDE)
+def test_norm_of_the_largest_and_the_smallest(zo, cols, rows, dtype):
+    """Rows whose squares leave fp32's range on either side, among ordinary ones (rows that share a wave among them):
+    rstd and y are as finite as the formula's.  eps is 0, so that nothing hides the small ones."""
+    if rows * cols > 3000000:
+        rows = 258
+    g = C.rng(109, rows, cols)
+    x, w = C.normal(g, rows, cols), (1 + 0.1 * C.normal(g, cols)).to(dtype)
+    big = torch.finfo(dtype).max
+    x[0] = big
+    x[1, cols // 2] = -big
+    x[2] *= 1e19
+    x[4] *= 1e-25
+    x[5] = 2.0 ** -120
+    x[6] *= 1e30
+    x[6, 0] = 1e-30
+    x[rows - 1] = -big
+    x = x.to(dtype)
+    rstd, y = C.rms_norm(x, w, 0.0)
+    oy, orr = Out(rows, cols, dtype), Out(rows, 1, F32)
+    oq, osc = Out(rows, cols, torch.uint8), Out(rows, 1, F32)
+    zo.zero_rms_norm(put(x), w.cuda(), 0.0, y=oy.view, rstd=orr.view, q8=oq.view, scale=osc.view)
+    torch.cuda.synchronize()
+    assert oy.guards_intact() and orr.guards_intact() and oq.guards_intact() and osc.guards_intact()
+    # a rstd below fp32's normal range is rounded to a multiple of 2^-149
+    off = (C.ROOT + 4 * C.U) * rstd + C.TINY[F32]
+    C.within(orr.view[:, 0], rstd, off, "rstd")
+    # and so are the two products of y
+    off = (C.ROOT + 8 * C.U + C.TINY[F32] / rstd)[:, None] * y.abs() + 4 * C.TINY[F32]
+    C.within(oy.view, y, C.rounded(off, y, dtype), "y")
+    C.check_e4m3(oq.view.contiguous(), y, 0, "q8")
+    # the backward of the same rows
+    dy = C.normal(g, rows, cols).to(dtype)
+    r32 = orr.view[:, 0].contiguous()
+    dx, dw, bx, bw = C.rms_norm_backward(dy, x, w, r32.cpu(), None)
+    ox, ow = Out(rows, cols, dtype), Out(1, cols, dtype)
+    room = Out(1, zo.zero_rms_norm_workspace(rows, cols), F32)
+    zo.zero_rms_norm_backward(put(dy), put(x), w.cuda(), r32, ox.view, ow.view[0], room.view[0])
+    torch.cuda.synchronize()
+    assert ox.guards_intact() and ow.guards_intact() and room.guards_intact()
+    # products below fp32's normal range each lose up to 2^-150
+    C.within(ox.view, dx, C.rounded(bx + 8 * C.TINY[F32], dx, dtype), "dx")
+    C.within(ow.view[0], dw, C.rounded(bw, dw, dtype), "dw")
+
+
+def test_norm_of_any_eps(zo):
+    """eps is a double: one below or above fp32's range counts as what it is."""
+    x = torch.zeros(3, 100)
+    x[1] = 1e-30
+    x[2] = 3.0
+    w = torch.ones(100)
+    for eps in (0.0, 1e-300, 1e-61, 1e-40, 1e-20, 1e20, 1e50, 1e70, 1e100):
+        y, rstd = torch.empty(3, 100, device="cuda"), torch.empty(3, device="cuda")
+        zo.zero_rms_norm(x.cuda(), w.cuda(), eps, y=y, rstd=rstd)
+        rd, yd = C.rms_norm(x, w, eps)
+        want, wy = rd.float().double(), (x.double() * rd.float().double()[:, None])
+        C.within(rstd, want, (C.ROOT + 4 * C.U) * rd.clamp(max=3.4e38) + 2 * C.TINY[F32], "rstd")
+        C.within(y, wy, C.rounded((C.ROOT + 8 * C.U) * wy.abs().nan_to_num(posinf=0.0), wy, F32), "y")
