@@ -242,3 +242,16 @@ def test_norm_of_any_eps(zo):
         want, wy = rd.float().double(), (x.double() * rd.float().double()[:, None])
         C.within(rstd, want, (C.ROOT + 4 * C.U) * rd.clamp(max=3.4e38) + 2 * C.TINY[F32], "rstd")
         C.within(y, wy, C.rounded((C.ROOT + 8 * C.U) * wy.abs().nan_to_num(posinf=0.0), wy, F32), "y")
+
+
+# --- shapes of the kernels that other tests' sizes do not reach ------------------------------
+
+@pytest.mark.parametrize("dtype", C.TYPES)
+@pytest.mark.parametrize("rows,cols", ((259, 1603), (258, 2041), (261, 1021), (257, 4089), (257, 2045), (259, 1100),
+                                       (258, 2048), (257, 4096), (300, 8200)))
+def test_norm_of_many_rows(zo, rows, cols, dtype):
+    """Above 256 rows, wide rows take four or two vectors a lane in place of a workgroup of 1024."""
+    for group in (0, 32, 256):
+        G.check_norm(zo, rows, cols, dtype, group)
+    G.check_norm(zo, rows, cols, dtype, 64, residual=False, pad=5, lead=3)
+    G.check_norm(zo, rows, cols, dtype, 128, pad=3, lead=1, in_place=True)
