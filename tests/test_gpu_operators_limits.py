@@ -255,3 +255,26 @@ def test_norm_of_many_rows(zo, rows, cols, dtype):
         G.check_norm(zo, rows, cols, dtype, group)
     G.check_norm(zo, rows, cols, dtype, 64, residual=False, pad=5, lead=3)
     G.check_norm(zo, rows, cols, dtype, 128, pad=3, lead=1, in_place=True)
+
+
+@pytest.mark.parametrize("dtype", C.TYPES)
+@pytest.mark.parametrize("score", ("softmax", "sigmoid"))
+@pytest.mark.parametrize("shape", ((33, 128, 8, 1, 1, 1), (9, 64, 12, 1, 1, 1), (9, 100, 20, 1, 1, 1),
+                                   (9, 512, 33, 1, 1, 1), (70, 128, 8, 4, 2, 2), (19, 112, 16, 8, 4, 2)))
+def test_route_of_middling_sizes(zo, shape, score, dtype):
+    """16 lanes a token with 4 and 8 keys, 32 with 4, 64 with 8."""
+    G.test_route(zo, shape, score, dtype)
+
+
+@pytest.mark.parametrize("dtype", C.TYPES)
+@pytest.mark.parametrize("score", ("softmax", "sigmoid"))
+@pytest.mark.parametrize("rows,experts,k", ((33, 128, 8), (9, 100, 20), (70, 72, 4)))
+def test_route_backward_of_middling_sizes(zo, rows, experts, k, score, dtype):
+    G.test_route_backward(zo, rows, experts, k, score, dtype)
+
+
+@pytest.mark.parametrize("dtype", C.TYPES)
+@pytest.mark.parametrize("vocab,k", ((3001, 16), (32003, 33), (60001, 64), (100277, 100)))
+def test_distill_of_more_vocabularies(zo, vocab, k, dtype):
+    """Shapes between the sizes of test_distill: 16-bit rows of 13 vectors a thread, fp32 rows of 4, 10 and 16."""
+    G.check_distill(zo, *G.distill_inputs(3, vocab, k, dtype, C.TYPES[vocab % 3], 113), tau=(1.0, 2.0, 1.5)[k % 3])
