@@ -278,3 +278,36 @@ def test_route_backward_of_middling_sizes(zo, rows, experts, k, score, dtype):
 def test_distill_of_more_vocabularies(zo, vocab, k, dtype):
     """Shapes between the sizes of test_distill: 16-bit rows of 13 vectors a thread, fp32 rows of 4, 10 and 16."""
     G.check_distill(zo, *G.distill_inputs(3, vocab, k, dtype, C.TYPES[vocab % 3], 113), tau=(1.0, 2.0, 1.5)[k % 3])
+
+
+def test_offsets_past_32_bits_of_the_other_calls(zo):
+    """As test_offsets_past_32_bits of test_gpu_operators.py, for the gradients, the routing and the loss alone: the same
+    bits as from rows that lie close together."""
+    ld, rows, cols = (1 << 31) + 64, 3, 512
+    buf = torch.zeros((rows - 1) * ld + 4 * cols, dtype=F16, device="cuda")
+    a, b, c, d = (torch.as_strided(buf, (rows, cols), (ld, 1), i * cols) for i in range(4))
+    near = [torch.randn(rows, cols, device="cuda").to(F16) for _ in range(3)]
+    for far, t in zip((a, b, c), near):
+        far.copy_(t)
+    w, rstd = torch.ones(cols, device="cuda", dtype=F16), torch.rand(rows, device="cuda") + 0.5
+    room, dw, dw2, out = torch.empty(4 * cols, device="cuda"), w.clone(), w.clone(), torch.empty_like(near[0])
+    zo.zero_rms_norm_backward(a, b, w, rstd, d, dw, room, dh=c)
+    zo.zero_rms_norm_backward(near[0], near[1], w, rstd, out, dw2, room, dh=near[2])
+    assert torch.equal(d, out) and torch.equal(dw, dw2)
+    index, index2 = (torch.empty(rows, 6, dtype=torch.int32, device="cuda") for _ in range(2))
+    weight, weight2 = (torch.empty(rows, 6, device="cuda") for _ in range(2))
+    zo.zero_route(a, index, weight)
+    zo.zero_route(near[0], index2, weight2)
+    assert torch.equal(index, index2) and torch.equal(weight, weight2)
+    for renorm in (True, False):
+        zo.zero_route_backward(a, index, weight, d, renormalise=renorm)
+        zo.zero_route_backward(near[0], index, weight, out, renormalise=renorm)
+        assert torch.equal(d, out)
+    idx, teacher = torch.arange(rows * 4, dtype=torch.int32, device="cuda").view(rows, 4), torch.rand(rows, 4, device="cuda")
+    loss, loss2, st, st2 = (torch.empty(rows, n, device="cuda") for n in (1, 1, 3, 3))
+    zo.zero_distill_loss(a, idx, teacher, loss, stats=st)
+    zo.zero_distill_loss(near[0], idx, teacher, loss2, stats=st2)
+    assert torch.equal(loss, loss2) and torch.equal(st, st2)
+    zo.zero_distill_backward(a, idx, teacher, st, d)
+    zo.zero_distill_backward(near[0], idx, teacher, st, out)
+    assert torch.equal(d, out)
