@@ -33,7 +33,9 @@
  *     that a call names as in place (same address, same ld).  Columns of one buffer
  *     (same ld) do not overlap.
  *   - Every array must lie inside one GPU-accessible allocation, checked on each
- *     call but while the stream is being captured (make one eager call first).
+ *     call but while the stream is being captured (make one eager call first). That
+ *     the current device can access it (its own memory, or a peer's with access enabled)
+ *     is the caller's to see to.
  *   - ZERO_EINVAL means that nothing was launched.
  */
 #ifndef ZERO_OPERATORS_H

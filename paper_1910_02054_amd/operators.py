@@ -4,7 +4,7 @@
 As in ``binding``: argument marshalling only, every operator runs in the library's HIP
 kernels, outputs are tensors of the caller's, calls only enqueue work on torch's current
 stream (or `stream`) and can be captured into a graph, and ZeroError carries the library's
-message.  Matrices are torch device tensors whose last dimension is contiguous; leading
+message.  Matrices are torch tensors on the current device whose last dimension is contiguous; leading
 dimensions are taken as one where their strides allow it, else the rows may be any stride
 apart.
 """
@@ -45,9 +45,22 @@ _lib.zero_route_workspace.argtypes = [_i64, _i32, ctypes.POINTER(_i64)]
 _raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
-def _on(stream):
-    """The hipStream_t of `stream`, or of torch's current stream on the current device."""
-    return _raw_stream(_device()) if stream is None else _stream(stream)
+def _on(stream, dev=None):
+    """The hipStream_t of `stream`, or of torch's current stream on the current device, which must be `dev`."""
+    here = _device()
+    if dev is not None and dev != here:
+        raise ValueError("the tensors are on device %d, the current device is %d" % (dev, here))
+    return _raw_stream(here) if stream is None else _stream(stream)
+
+
+def _place(t, what, dev=None):
+    """The device of a tensor; with `dev`, which it is not on, the error that says so."""
+    at = t.get_device()
+    if at < 0:
+        raise TypeError("%s must be a device tensor" % what)
+    if dev is not None:
+        raise ValueError("%s is on device %d, other tensors of the call on device %d" % (what, at, dev))
+    return at
 
 
 def _type(t, what):
@@ -68,14 +81,15 @@ def _sizes(t, what):
     return torch.Size((t.numel() // n if n else 0, n))
 
 
-def _matrix(t, dtype, what, size):
-    """(address, elements from row to row) of a device matrix of the given type and size; (0, cols) for None."""
+def _matrix(t, dtype, what, size, dev):
+    """(address, elements from row to row) of a matrix of the given type and size on device `dev`; (0, cols) for
+    None."""
     if t is None:
         return 0, size[1]
     if t.dtype is not dtype:
         raise TypeError("%s: dtype %s, not %s" % (what, t.dtype, dtype))
-    if not t.is_cuda:
-        raise TypeError("%s must be a device tensor" % what)
+    if t.get_device() != dev:
+        _place(t, what, dev)
     if t.shape != size:
         if _sizes(t, what) != size:
             raise ValueError("%s has shape %s, not %s" % (what, list(t.shape), list(size)))
@@ -87,14 +101,14 @@ def _matrix(t, dtype, what, size):
     return t.data_ptr(), step if rows > 1 else cols
 
 
-def _vector(t, dtype, what, numel):
-    """The address of a contiguous device array of `numel` elements (0 for None)."""
+def _vector(t, dtype, what, numel, dev):
+    """The address of a contiguous array of `numel` elements on device `dev` (0 for None)."""
     if t is None:
         return 0
     if t.dtype is not dtype:
         raise TypeError("%s: dtype %s, not %s" % (what, t.dtype, dtype))
-    if not t.is_cuda:
-        raise TypeError("%s must be a device tensor" % what)
+    if t.get_device() != dev:
+        _place(t, what, dev)
     if not t.is_contiguous():
         raise TypeError("%s must be contiguous" % what)
     if t.numel() != numel:
@@ -102,9 +116,9 @@ def _vector(t, dtype, what, numel):
     return t.data_ptr()
 
 
-def _room(t, dtype, what):
+def _room(t, dtype, what, dev):
     """(address, elements) of a workspace, which may be None."""
-    return (0, 0) if t is None else (_vector(t, dtype, what, t.numel()), t.numel())
+    return (0, 0) if t is None else (_vector(t, dtype, what, t.numel(), dev), t.numel())
 
 
 _F32, _I32 = torch.float32, torch.int32
@@ -117,19 +131,21 @@ def zero_rms_norm(x, weight, eps, residual=None, h=None, y=None, q8=None, scale=
     Each output is written where a tensor is given; y, q8 * scale and h are [rows, cols], rstd [rows],
     scale [rows, ceil(cols / group)].  h may be residual or x in place, and so may y."""
     code, dt = _type(x, "x"), x.dtype
+    dev = _place(x, "x")
     size = rows, cols = _sizes(x, "x")
-    px, ld_x = _matrix(x, dt, "x", size)
-    pr, ld_r = _matrix(residual, dt, "residual", size)
-    ph, ld_h = _matrix(h, dt, "h", size)
-    py, ld_y = _matrix(y, dt, "y", size)
+    px, ld_x = _matrix(x, dt, "x", size, dev)
+    pr, ld_r = _matrix(residual, dt, "residual", size, dev)
+    ph, ld_h = _matrix(h, dt, "h", size, dev)
+    py, ld_y = _matrix(y, dt, "y", size, dev)
     pq, ld_q, ps = 0, cols, 0
     if q8 is not None:
-        pq, ld_q = _matrix(q8, torch.uint8 if q8.dtype is torch.uint8 else torch.float8_e4m3fn, "q8", size)
+        pq, ld_q = _matrix(q8, torch.uint8 if q8.dtype is torch.uint8 else torch.float8_e4m3fn, "q8", size, dev)
     if scale is not None:
-        ps = _vector(scale, _F32, "scale", rows * (-(-cols // group) if group > 0 else 1))
-    args = RMS_NORM_ARGS.pack(code, group, rows, cols, eps, px, ld_x, pr, ld_r, _vector(weight, dt, "weight", cols), ph, ld_h,
-                       py, ld_y, pq, ld_q, ps, _vector(rstd, _F32, "rstd", rows))
-    rc = _lib.zero_rms_norm(args, _on(stream))
+        ps = _vector(scale, _F32, "scale", rows * (-(-cols // group) if group > 0 else 1), dev)
+    pw, prs = _vector(weight, dt, "weight", cols, dev), _vector(rstd, _F32, "rstd", rows, dev)
+    args = RMS_NORM_ARGS.pack(code, group, rows, cols, eps, px, ld_x, pr, ld_r, pw, ph, ld_h, py, ld_y, pq, ld_q, ps,
+                              prs)
+    rc = _lib.zero_rms_norm(args, _on(stream, dev))
     if rc < 0:
         _check(rc)
 
@@ -147,16 +163,17 @@ def zero_rms_norm_backward(dy, h, weight, rstd, dx, dweight, workspace=None, dh=
     gradient dh that reaches h from elsewhere.  workspace: a float32 tensor of at least
     zero_rms_norm_workspace(rows, cols) elements."""
     code, dt = _type(h, "h"), h.dtype
+    dev = _place(h, "h")
     size = rows, cols = _sizes(h, "h")
-    ph, ld_h = _matrix(h, dt, "h", size)
-    pdy, ld_dy = _matrix(dy, dt, "dy", size)
-    pdh, ld_dh = _matrix(dh, dt, "dh", size)
-    pdx, ld_dx = _matrix(dx, dt, "dx", size)
-    pw, n = _room(workspace, _F32, "workspace")
-    args = RMS_NORM_BACKWARD_ARGS.pack(code, 0, rows, cols, pdy, ld_dy, ph, ld_h, _vector(weight, dt, "weight", cols),
-                               _vector(rstd, _F32, "rstd", rows), pdh, ld_dh, pdx, ld_dx,
-                               _vector(dweight, dt, "dweight", cols), pw, n)
-    rc = _lib.zero_rms_norm_backward(args, _on(stream))
+    ph, ld_h = _matrix(h, dt, "h", size, dev)
+    pdy, ld_dy = _matrix(dy, dt, "dy", size, dev)
+    pdh, ld_dh = _matrix(dh, dt, "dh", size, dev)
+    pdx, ld_dx = _matrix(dx, dt, "dx", size, dev)
+    pw, n = _room(workspace, _F32, "workspace", dev)
+    args = RMS_NORM_BACKWARD_ARGS.pack(code, 0, rows, cols, pdy, ld_dy, ph, ld_h,
+                                       _vector(weight, dt, "weight", cols, dev), _vector(rstd, _F32, "rstd", rows, dev),
+                                       pdh, ld_dh, pdx, ld_dx, _vector(dweight, dt, "dweight", cols, dev), pw, n)
+    rc = _lib.zero_rms_norm_backward(args, _on(stream, dev))
     if rc < 0:
         _check(rc)
 
@@ -174,13 +191,14 @@ def zero_route(logits, index, weight, score="softmax", bias=None, groups=1, top_
     [tokens, k], in falling order of the keys.  score: "softmax" or "sigmoid"; bias [experts] float32 acts on the
     choice alone; groups > 1 keeps the top_groups groups of the largest sums of their group_top largest keys."""
     code = _type(logits, "logits")
+    dev = _place(logits, "logits")
     size = rows, experts = _sizes(logits, "logits")
-    pl, ld = _matrix(logits, logits.dtype, "logits", size)
+    pl, ld = _matrix(logits, logits.dtype, "logits", size, dev)
     k = index.shape[-1]
-    args = ROUTE_ARGS.pack(code, _score(score), rows, experts, k, groups, top_groups, group_top, bool(renormalise), scale,
-                     pl, ld, _vector(bias, _F32, "bias", experts), _vector(index, _I32, "index", rows * k),
-                     _vector(weight, _F32, "weight", rows * k))
-    rc = _lib.zero_route(args, _on(stream))
+    args = ROUTE_ARGS.pack(code, _score(score), rows, experts, k, groups, top_groups, group_top, bool(renormalise),
+                           scale, pl, ld, _vector(bias, _F32, "bias", experts, dev),
+                           _vector(index, _I32, "index", rows * k, dev), _vector(weight, _F32, "weight", rows * k, dev))
+    rc = _lib.zero_route(args, _on(stream, dev))
     if rc < 0:
         _check(rc)
 
@@ -196,11 +214,12 @@ def zero_route_order(index, experts, offsets, order, workspace=None, stream=None
     """The slots (flat positions in index, int32) by expert, then by slot: order[offsets[e]:offsets[e + 1]] are
     expert e's; slots without an expert are left out and order ends in as many -1.  offsets [experts + 1] and order
     [slots] are int32; workspace: int32, at least zero_route_workspace(slots, experts) elements."""
-    n = index.numel()
-    pw, room = _room(workspace, _I32, "workspace")
-    args = ROUTE_ORDER_ARGS.pack(_vector(index, _I32, "index", n), n, experts, 0,
-                          _vector(offsets, _I32, "offsets", experts + 1), _vector(order, _I32, "order", n), pw, room)
-    rc = _lib.zero_route_order(args, _on(stream))
+    n, dev = index.numel(), _place(index, "index")
+    pw, room = _room(workspace, _I32, "workspace", dev)
+    args = ROUTE_ORDER_ARGS.pack(_vector(index, _I32, "index", n, dev), n, experts, 0,
+                                 _vector(offsets, _I32, "offsets", experts + 1, dev),
+                                 _vector(order, _I32, "order", n, dev), pw, room)
+    rc = _lib.zero_route_order(args, _on(stream, dev))
     if rc < 0:
         _check(rc)
 
@@ -210,14 +229,16 @@ def zero_route_backward(logits, index, dweight, dlogits, score="softmax", bias=N
     """The gradient of zero_route's logits into dlogits [tokens, experts] (may be logits in place) from that of its
     weights, dweight [tokens, k] float32, and its index."""
     code, dt = _type(logits, "logits"), logits.dtype
+    dev = _place(logits, "logits")
     size = rows, experts = _sizes(logits, "logits")
-    pl, ld = _matrix(logits, dt, "logits", size)
-    pd, ld_d = _matrix(dlogits, dt, "dlogits", size)
+    pl, ld = _matrix(logits, dt, "logits", size, dev)
+    pd, ld_d = _matrix(dlogits, dt, "dlogits", size, dev)
     k = index.shape[-1]
     args = ROUTE_BACKWARD_ARGS.pack(code, _score(score), rows, experts, k, bool(renormalise), 0, scale, pl, ld,
-                             _vector(bias, _F32, "bias", experts), _vector(index, _I32, "index", rows * k),
-                             _vector(dweight, _F32, "dweight", rows * k), pd, ld_d)
-    rc = _lib.zero_route_backward(args, _on(stream))
+                                    _vector(bias, _F32, "bias", experts, dev),
+                                    _vector(index, _I32, "index", rows * k, dev),
+                                    _vector(dweight, _F32, "dweight", rows * k, dev), pd, ld_d)
+    rc = _lib.zero_route_backward(args, _on(stream, dev))
     if rc < 0:
         _check(rc)
 
@@ -225,20 +246,22 @@ def zero_route_backward(logits, index, dweight, dlogits, score="softmax", bias=N
 def _distill(fn, logits, teacher_index, teacher_logits, loss, stats, dlogits, dloss, labels, soft, hard, temperature,
              row_weight, grad_scale, stream):
     code, dt = _type(logits, "logits"), logits.dtype
+    dev = _place(logits, "logits")
     size = rows, vocab = _sizes(logits, "logits")
-    pl, ld = _matrix(logits, dt, "logits", size)
-    pd, ld_d = _matrix(dlogits, dt, "dlogits", size)
+    pl, ld = _matrix(logits, dt, "logits", size, dev)
+    pd, ld_d = _matrix(dlogits, dt, "dlogits", size, dev)
     k, teacher, pi, pt = 0, ZERO_F32, 0, 0
     if teacher_index is not None:
         k = teacher_index.shape[-1]
         teacher = _type(teacher_logits, "teacher_logits")
-        pi = _vector(teacher_index, _I32, "teacher_index", rows * k)
-        pt = _vector(teacher_logits, teacher_logits.dtype, "teacher_logits", rows * k)
+        pi = _vector(teacher_index, _I32, "teacher_index", rows * k, dev)
+        pt = _vector(teacher_logits, teacher_logits.dtype, "teacher_logits", rows * k, dev)
     args = DISTILL_ARGS.pack(code, teacher, rows, vocab, k, 0, temperature, soft, hard, grad_scale, pl, ld, pi, pt,
-                       _vector(labels, _I32, "labels", rows), _vector(row_weight, _F32, "row_weight", rows),
-                       _vector(loss, _F32, "loss", rows), _vector(stats, _F32, "stats", 3 * rows),
-                       _vector(dloss, _F32, "dloss", rows), pd, ld_d)
-    rc = fn(args, _on(stream))
+                             _vector(labels, _I32, "labels", rows, dev),
+                             _vector(row_weight, _F32, "row_weight", rows, dev), _vector(loss, _F32, "loss", rows, dev),
+                             _vector(stats, _F32, "stats", 3 * rows, dev), _vector(dloss, _F32, "dloss", rows, dev),
+                             pd, ld_d)
+    rc = fn(args, _on(stream, dev))
     if rc < 0:
         _check(rc)
 
