@@ -46,21 +46,25 @@ _raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDev
 
 
 def _on(stream, dev=None):
-    """The hipStream_t of `stream`, or of torch's current stream on the current device, which must be `dev`."""
-    here = _device()
-    if dev is not None and dev != here:
-        raise ValueError("the tensors are on device %d, the current device is %d" % (dev, here))
-    return _raw_stream(here) if stream is None else _stream(stream)
-
-
-def _place(t, what, dev=None):
-    """The device of a tensor; with `dev`, which it is not on, the error that says so."""
-    at = t.get_device()
-    if at < 0:
-        raise TypeError("%s must be a device tensor" % what)
+    """The hipStream_t of `stream`, or of torch's current stream on the current device, which must be `dev`, the
+    device of a call's tensors."""
     if dev is not None:
-        raise ValueError("%s is on device %d, other tensors of the call on device %d" % (what, at, dev))
-    return at
+        if dev < 0:
+            raise TypeError("a call's arrays must be device tensors")
+        here = _device()
+        if dev != here:
+            raise ValueError("the tensors are on device %d, the current device is %d" % (dev, here))
+        if stream is None:
+            return _raw_stream(here)
+    return _raw_stream(_device()) if stream is None else _stream(stream)
+
+
+def _elsewhere(t, what, dev):
+    """The error of a tensor that is not on `dev`, where the call's first one is (-1: the host)."""
+    at = t.get_device()
+    if at < 0 or dev < 0:
+        return TypeError("%s: a call's arrays must be device tensors" % what)
+    return ValueError("%s is on device %d, other tensors of the call on device %d" % (what, at, dev))
 
 
 def _type(t, what):
@@ -89,7 +93,7 @@ def _matrix(t, dtype, what, size, dev):
     if t.dtype is not dtype:
         raise TypeError("%s: dtype %s, not %s" % (what, t.dtype, dtype))
     if t.get_device() != dev:
-        _place(t, what, dev)
+        raise _elsewhere(t, what, dev)
     if t.shape != size:
         if _sizes(t, what) != size:
             raise ValueError("%s has shape %s, not %s" % (what, list(t.shape), list(size)))
@@ -108,7 +112,7 @@ def _vector(t, dtype, what, numel, dev):
     if t.dtype is not dtype:
         raise TypeError("%s: dtype %s, not %s" % (what, t.dtype, dtype))
     if t.get_device() != dev:
-        _place(t, what, dev)
+        raise _elsewhere(t, what, dev)
     if not t.is_contiguous():
         raise TypeError("%s must be contiguous" % what)
     if t.numel() != numel:
@@ -131,7 +135,7 @@ def zero_rms_norm(x, weight, eps, residual=None, h=None, y=None, q8=None, scale=
     Each output is written where a tensor is given; y, q8 * scale and h are [rows, cols], rstd [rows],
     scale [rows, ceil(cols / group)].  h may be residual or x in place, and so may y."""
     code, dt = _type(x, "x"), x.dtype
-    dev = _place(x, "x")
+    dev = x.get_device()
     size = rows, cols = _sizes(x, "x")
     px, ld_x = _matrix(x, dt, "x", size, dev)
     pr, ld_r = _matrix(residual, dt, "residual", size, dev)
@@ -163,7 +167,7 @@ def zero_rms_norm_backward(dy, h, weight, rstd, dx, dweight, workspace=None, dh=
     gradient dh that reaches h from elsewhere.  workspace: a float32 tensor of at least
     zero_rms_norm_workspace(rows, cols) elements."""
     code, dt = _type(h, "h"), h.dtype
-    dev = _place(h, "h")
+    dev = h.get_device()
     size = rows, cols = _sizes(h, "h")
     ph, ld_h = _matrix(h, dt, "h", size, dev)
     pdy, ld_dy = _matrix(dy, dt, "dy", size, dev)
@@ -191,7 +195,7 @@ def zero_route(logits, index, weight, score="softmax", bias=None, groups=1, top_
     [tokens, k], in falling order of the keys.  score: "softmax" or "sigmoid"; bias [experts] float32 acts on the
     choice alone; groups > 1 keeps the top_groups groups of the largest sums of their group_top largest keys."""
     code = _type(logits, "logits")
-    dev = _place(logits, "logits")
+    dev = logits.get_device()
     size = rows, experts = _sizes(logits, "logits")
     pl, ld = _matrix(logits, logits.dtype, "logits", size, dev)
     k = index.shape[-1]
@@ -214,7 +218,7 @@ def zero_route_order(index, experts, offsets, order, workspace=None, stream=None
     """The slots (flat positions in index, int32) by expert, then by slot: order[offsets[e]:offsets[e + 1]] are
     expert e's; slots without an expert are left out and order ends in as many -1.  offsets [experts + 1] and order
     [slots] are int32; workspace: int32, at least zero_route_workspace(slots, experts) elements."""
-    n, dev = index.numel(), _place(index, "index")
+    n, dev = index.numel(), index.get_device()
     pw, room = _room(workspace, _I32, "workspace", dev)
     args = ROUTE_ORDER_ARGS.pack(_vector(index, _I32, "index", n, dev), n, experts, 0,
                                  _vector(offsets, _I32, "offsets", experts + 1, dev),
@@ -229,7 +233,7 @@ def zero_route_backward(logits, index, dweight, dlogits, score="softmax", bias=N
     """The gradient of zero_route's logits into dlogits [tokens, experts] (may be logits in place) from that of its
     weights, dweight [tokens, k] float32, and its index."""
     code, dt = _type(logits, "logits"), logits.dtype
-    dev = _place(logits, "logits")
+    dev = logits.get_device()
     size = rows, experts = _sizes(logits, "logits")
     pl, ld = _matrix(logits, dt, "logits", size, dev)
     pd, ld_d = _matrix(dlogits, dt, "dlogits", size, dev)
@@ -246,7 +250,7 @@ def zero_route_backward(logits, index, dweight, dlogits, score="softmax", bias=N
 def _distill(fn, logits, teacher_index, teacher_logits, loss, stats, dlogits, dloss, labels, soft, hard, temperature,
              row_weight, grad_scale, stream):
     code, dt = _type(logits, "logits"), logits.dtype
-    dev = _place(logits, "logits")
+    dev = logits.get_device()
     size = rows, vocab = _sizes(logits, "logits")
     pl, ld = _matrix(logits, dt, "logits", size, dev)
     pd, ld_d = _matrix(dlogits, dt, "dlogits", size, dev)
