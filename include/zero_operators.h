@@ -25,7 +25,8 @@
  *     They write all of every output and read no output's old contents.
  *   - `dtype` is the type of a record's arrays declared void* (ZERO_F32,
  *     ZERO_F16, ZERO_BF16).  Arithmetic is in fp32 whatever the type, each output
- *     is rounded once, to nearest even.
+ *     is rounded once, to nearest even.  A softmax's terms below 2^-126 count as 0, and so
+ *     do gradients that are their multiples, whatever the loss scale.
  *   - A matrix [rows, cols] has its rows `ld` elements apart (ld >= cols; any
  *     alignment of an element, rows of whole 16-byte groups run fastest); its
  *     other elements are neither read nor written.  rows may be 0.
@@ -135,7 +136,10 @@ int zero_rms_norm_workspace(int64_t rows, int64_t cols, int64_t* floats);
 /* Each token takes the k experts with the largest keys, equal keys by the lowest
  * expert, in falling order:
  *   sigmoid: key = 1 / (1 + exp(-logit)) + bias
- *   softmax: key = logit + bias (the order of exp(bias) * softmax)
+ *   softmax: key = logit + bias, the order of exp(bias) * softmax.  (Loss-free balancing as it
+ *            is published adds the bias to the probability: softmax + bias.  Where biases differ
+ *            that rule can choose other experts, and a bias trained for one does not serve the
+ *            other.  group_top = 2 likewise adds two keys, not two probabilities.)
  * The bias balances the experts' loads: it acts on the choice alone.  An expert
  * is out where its logit or its bias is -inf: it is neither chosen nor part of a sum.
  * With groups > 1 the experts are cut into that many equal runs; a group's score

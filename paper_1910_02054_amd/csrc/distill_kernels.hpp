@@ -15,9 +15,12 @@
 // every vector costs more than the few lines that are written twice; 4096 rows of 50304
 // f16 with 64 entries 155 us in place of 144.)
 //
-// Bound by HBM: 4096 rows of 50257 f16, 64 entries, both terms, 143 us, 5.8 TB/s (a second exponential an element, for
-// temperatures other than 1 and 2 with a hard term, 154); 1024 of 131072 bf16 107 us, 5.0: such a row leaves
-// one workgroup a compute unit; 65536 of 2048 f16 111 us, 5.1; the loss alone of 4096 of 50257 70 us, 5.9.
+// Bound by HBM, with the vector ALU not far behind: 4096 rows of 50257 f16, 64 entries, both terms,
+// 143 us, 5.8 TB/s, the ALU busy for 0.69 of it.  With a second exponential an element (temperatures
+// other than 1 and 2 with a hard term) 151, and up to 185 in calls that follow one another for longer
+// than 1.5 ms, when the clock falls.  1024 of 131072 bf16 108 us, 5.0 TB/s: such a row leaves one
+// workgroup a compute unit; 65536 of 2048 f16 112 us, 5.0; 2048 of 50257 f32 145, 5.7; the loss
+// alone of 4096 of 50257 f16 69 us, 6.0.
 #pragma once
 
 #include "row_ops.hpp"
@@ -93,9 +96,9 @@ struct Against {
 
 constexpr int kBatch = 4;  // vectors at a time of a row that is read as it is needed
 
-// Whether a row goes past the caches: long ones, which do not come back (4096 of 50304 f16 144 us in place of 155, of
-// 32000 101 in place of 113); the tokens' values, written after the rest of a row, find short rows' lines still
-// in L2 (16384 of 8192: 111 us, 137 to 178 past it).
+// Whether a row goes past the caches: long ones, which do not come back (4096 of 50304 f16 142 us in place of 154, of
+// 32000 96 in place of 104); the tokens' values, written after the rest of a row, find short rows' lines still
+// in L2 (16384 of 8192: 110 us, 176 past it; 65536 of 2048: 112, 163).
 constexpr bool past_caches(int threads, int vectors) { return vectors == 0 || threads * vectors > 1024; }
 
 // How the soft and the hard term share the exponentials of an element.
@@ -331,9 +334,10 @@ __device__ __forceinline__ void distill_row(const zero_distill_args_t& a, const 
     sum = seg_reduce<64>(sum, Add());
     const float over = has_soft ? 1.f / sum : 0.f;
 
-    // log p_j - log q_tau[token_j] = ((t_j - top) - (z_j - m) + tau ln 2 (log2 S - log2 sum)) / tau, so with tau^2 before
-    // it a term is a difference of logits (and a few bits of the sums) times tau: nothing in it leaves fp32 before
-    // the loss does, whatever the temperature and also where the student holds the type's lowest value.
+    // log p_j - log q_tau[token_j] = ((t_j - top) - (z_j - m) + tau ln 2 (log2 S - log2 sum)) / tau, so with
+    // tau^2 before it a term is a difference of logits (and a few bits of the sums) times tau: nothing in it
+    // leaves fp32 before the loss does, whatever the temperature and also where the student holds the
+    // type's lowest value.
     if constexpr (MODE != kDistillBack) {
         if (wave == 0) {
             const float bits = k.bit * (x.log_sum(s) - log2_fast(sum));
@@ -436,7 +440,7 @@ __device__ __forceinline__ void distill_row(const zero_distill_args_t& a, const 
 }
 
 // Waves a SIMD: all eight while the packed row leaves room in 64 registers, six of short workgroups with eight vectors
-// a thread (at eight they spill: 8192 rows of 11093 bf16 82 us in place of 80), and one workgroup of 1024 a
+// a thread (at eight they spill: 8192 rows of 11093 bf16 74 us in place of 72), and one workgroup of 1024 a
 // compute unit above that.
 template <typename T, int NT, int NV, int MODE>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NV <= 7 ? 8 : NT < 1024 ? 6 : 4))) void k_distill(

@@ -4,16 +4,18 @@
 //   h = x + r (rounded),  rstd = (mean h^2 + eps)^(-1/2),  y = h rstd w
 //   dx = rstd (g - n mean(g n)) + dh,  g = dy w,  n = h rstd;  dw = sum over rows of dy n
 //
-// Both are bound by HBM: an element costs 6 to 18 bytes and about ten operations.  A
-// row is read once and stays in registers between its reduction and its output:
-// LPR lanes hold a row, NV 16-byte vectors each.  LPR is a sixteenth of a wave's
-// row of lanes up to a workgroup of 1024, the smallest for which NV stays small, so that short
-// rows share a wave and need no barrier, and long ones are spread over enough
-// waves to keep the loads in flight.
+// Both are bound by HBM: an element costs 6 to 18 bytes and 30 to 42 vector instructions (42 with
+// e4m3 rows, which keep the vector ALU busy for 0.7 of the time).  A row is read once and stays in
+// registers between its reduction and its output: LPR lanes hold a row, NV 16-byte vectors each.
+// LPR goes from 16 lanes of a wave to a workgroup of 1024, the smallest for which NV
+// stays small, so that short rows share a wave and need no barrier, and long ones are spread over
+// enough waves to keep the loads in flight.
 //
-// Measured: 16384 rows of 8192 bf16 with the residual, both outputs and e4m3 in groups of 128, 206 us, 5.9
-// TB/s; 16384 of 4096 f16 to e4m3 95 us, 6.4; the gradient of 8192 of 4096 f16 49 us, 5.5 TB/s, and 4.6
-// for the partial sums' kernel; one row of 8192 3.6 us.  (The copy kernel reaches 6.7 TB/s.)
+// Measured: 16384 rows of 8192 bf16 with the residual, both outputs and e4m3 in groups of 128, 209 us,
+// 5.8 TB/s; 16384 of 4096 f16 with a scale a row 95 us, 6.4; 8192 of 8192 f32 without e4m3 179 us, 6.0;
+// the gradient of 8192 of 4096 f16 49 us, 5.5 TB/s, and 4.6 for the partial sums' kernel; one row of
+// 8192 3.7 us.  (The copy kernel reaches 6.7 TB/s.)  The gradient of f32 rows above 16384 columns
+// spills 45 registers a lane: 2048 of 25600 197 us, 4.3 TB/s.
 #pragma once
 
 #include "row_ops.hpp"
@@ -51,8 +53,8 @@ __device__ __forceinline__ void store_e4m3(uint8_t* p, const float* f) {
 // y / scale, rounded once, for many y of one scale t: the product with the rounded reciprocal is off by up
 // to two roundings, which puts a quotient beside a midpoint of two codes (bf16 rows have many on one) on the other
 // side; the exact remainder of that product corrects it to the nearest fp32.  The remainder has
-// bits down to 2^-34 t ulp(1) where the code is not 0, so scales below 1 (least: 2^-100 / 448) are raised by 2^24 with their y.
-// An infinite scale leaves 0 of what is finite, and of -0 stays -0.
+// bits down to 2^-34 t ulp(1) where the code is not 0, so scales below 1 (least: 2^-100 / 448) are
+// raised by 2^24 with their y.  An infinite scale leaves 0 of what is finite, and of -0 stays -0.
 struct Quotient {
     float k, t, inv;
     __device__ __forceinline__ explicit Quotient(float scale) : k(scale < 1.f ? 0x1p24f : 1.f) {
@@ -112,14 +114,14 @@ struct Held {
     }
 };
 
-// Rows of more than 64 vectors go past the caches: 4096 rows of 1600 f16 9.7 us in place of 11.5,
-// 16384 of 4096 95 in place of 108; rows of 512 lose by it (13.6, 12.7).
+// Rows of more than 64 vectors go past the caches: 4096 rows of 1600 f16 9.9 us in place of 11.4, 16384 of
+// 4096 with e4m3 95 in place of 108; rows of 512 gain nothing (14.0, 14.4 past them).
 constexpr bool norm_past(int lpr, int nv) { return lpr * nv > 64; }
 
-// The reciprocal root of a row whose sum of squares, or eps, has left fp32's range (or is so small that squares are lost): the
-// squares again, of elements scaled by 2^-80 or 2^80, and the rest in fp64.  A row that holds an infinity or a
-// NaN comes out as it went in.  `total` is the mean and eps in fp32, which tells such rows: where it lies in
-// [2^-85, inf) all that was lost is below 2^-49 of it.
+// The reciprocal root of a row whose sum of squares, or eps, has left fp32's range (or is so small that
+// squares are lost): the squares again, of elements scaled by 2^-80 or 2^80, and the rest in fp64.  A row
+// that holds an infinity or a NaN comes out as it went in.  `total` is the mean and eps in fp32, which
+// tells such rows: where it lies in [2^-85, inf) all that was lost is below 2^-49 of it.
 constexpr float kLeastTotal = 0x1p-85f;
 
 template <int LPR, typename F>
