@@ -18,9 +18,9 @@
 // Bound by HBM, with the vector ALU not far behind: 4096 rows of 50257 f16, 64 entries, both terms,
 // 143 us, 5.8 TB/s, the ALU busy for 0.69 of it.  With a second exponential an element (temperatures
 // other than 1 and 2 with a hard term) 151, and up to 185 in calls that follow one another for longer
-// than 1.5 ms, when the clock falls.  1024 of 131072 bf16 108 us, 5.0 TB/s: such a row leaves one
-// workgroup a compute unit; 65536 of 2048 f16 112 us, 5.0; 2048 of 50257 f32 145, 5.7; the loss
-// alone of 4096 of 50257 f16 69 us, 6.0.
+// than 1.5 ms, when the clock falls.  1024 of 131072 bf16 109 us, 5.0 TB/s: such a row leaves one
+// workgroup a compute unit; 65536 of 2048 f16 114 us, 4.9; 2048 of 50257 f32 148, 5.6; the loss
+// alone of 4096 of 50257 f16 72 us, 5.7.
 #pragma once
 
 #include "row_ops.hpp"
@@ -96,9 +96,9 @@ struct Against {
 
 constexpr int kBatch = 4;  // vectors at a time of a row that is read as it is needed
 
-// Whether a row goes past the caches: long ones, which do not come back (4096 of 50304 f16 142 us in place of 154, of
+// Whether a row goes past the caches: long ones, which do not come back (4096 of 50304 f16 144 us in place of 154, of
 // 32000 96 in place of 104); the tokens' values, written after the rest of a row, find short rows' lines still
-// in L2 (16384 of 8192: 110 us, 176 past it; 65536 of 2048: 112, 163).
+// in L2 (16384 of 8192: 110 us, 176 past it; 65536 of 2048: 114, 163).
 constexpr bool past_caches(int threads, int vectors) { return vectors == 0 || threads * vectors > 1024; }
 
 // How the soft and the hard term share the exponentials of an element.

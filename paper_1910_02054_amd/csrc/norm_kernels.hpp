@@ -11,11 +11,11 @@
 // stays small, so that short rows share a wave and need no barrier, and long ones are spread over
 // enough waves to keep the loads in flight.
 //
-// Measured: 16384 rows of 8192 bf16 with the residual, both outputs and e4m3 in groups of 128, 209 us,
-// 5.8 TB/s; 16384 of 4096 f16 with a scale a row 95 us, 6.4; 8192 of 8192 f32 without e4m3 179 us, 6.0;
+// Measured: 16384 rows of 8192 bf16 with the residual, both outputs and e4m3 in groups of 128, 212 us,
+// 5.7 TB/s; 16384 of 4096 f16 with a scale a row 95 us, 6.4; 8192 of 8192 f32 without e4m3 174 us, 6.2;
 // the gradient of 8192 of 4096 f16 49 us, 5.5 TB/s, and 4.6 for the partial sums' kernel; one row of
-// 8192 3.7 us.  (The copy kernel reaches 6.7 TB/s.)  The gradient of f32 rows above 16384 columns
-// spills 45 registers a lane: 2048 of 25600 197 us, 4.3 TB/s.
+// 8192 3.8 us.  (The copy kernel reaches 6.7 TB/s.)  The gradient of f32 rows above 16384 columns
+// spills 45 registers a lane: 2048 of 25600 195 us, 4.3 TB/s.
 #pragma once
 
 #include "row_ops.hpp"
@@ -114,8 +114,8 @@ struct Held {
     }
 };
 
-// Rows of more than 64 vectors go past the caches: 4096 rows of 1600 f16 9.9 us in place of 11.4, 16384 of
-// 4096 with e4m3 95 in place of 108; rows of 512 gain nothing (14.0, 14.4 past them).
+// Rows of more than 64 vectors go past the caches: 4096 rows of 1600 f16 10.0 us in place of 11.4, 16384 of
+// 4096 with e4m3 95 in place of 108; rows of 512 lose by it (13.3, 14.4).
 constexpr bool norm_past(int lpr, int nv) { return lpr * nv > 64; }
 
 // The reciprocal root of a row whose sum of squares, or eps, has left fp32's range (or is so small that

@@ -7,9 +7,9 @@
 // run side by side.  A lane's experts are a run of neighbours inside one group, runs
 // rising with the lane, so the lowest lane that holds the maximum holds the lowest such expert.
 //
-// Measured at 16384 tokens of 256 experts (8 of them from 4 of 8 groups, sigmoid, bias): 15.8 us, of which a round takes
-// 0.7, the sigmoids 2.7 and the groups 2 (the logits' 17 MB are 2.5 us at the copy kernel's rate); the ordering of their
-// slots 3.0 and 8.0 in two launches; the gradient 8.7, softmax over all experts 15.0 (below).
+// Measured at 16384 tokens of 256 experts (8 of them from 4 of 8 groups, sigmoid, bias): 15.9 us, of which a round takes
+// 0.7, the sigmoids 2.7 and the groups 1.6 (the logits' 17 MB are 2.5 us at the copy kernel's rate); the ordering of their
+// slots 3.6 and 7.9 in two launches; the gradient 8.9, softmax over all experts 15.2 (below).
 #pragma once
 
 #include "row_ops.hpp"
@@ -380,10 +380,10 @@ __global__ __launch_bounds__(kOrderBlock) void k_route_order(const int32_t* inde
 
 // ---------------------------------------------------------------------------
 // Gradient of the logits: the row goes through LDS, where the chosen experts' few terms are
-// put between zeros, and out in whole vectors.  Of the 8.7 us at 16384 tokens of 256 f32 experts the
+// put between zeros, and out in whole vectors.  Of the 8.9 us at 16384 tokens of 256 f32 experts the
 // rows' bytes are 2.5; the rest is a token's chain of latencies: index, gathered logit, sums across the lanes,
 // LDS and its two barriers, then the first store.  Softmax over all experts reads the row three
-// times, from the caches after the first: 15.0 us.
+// times, from the caches after the first: 15.2 us.
 // ---------------------------------------------------------------------------
 template <typename T, int LPT>
 __global__ __launch_bounds__(kRouteBlock) void k_route_back(const zero_route_backward_args_t a, int64_t first) {

@@ -173,7 +173,7 @@ int with_type(int dtype, F f) {
 // ---------------------------------------------------------------------------
 // Norm.  The lanes of a row and its vectors a lane, from the row's 16-byte vectors: lanes of one
 // wave while they hold the row in four vectors, then a workgroup, and of 1024 where that leaves a lane
-// one vector or the rows are too few to fill the device otherwise (one row of 8192 f16 3.7 us, 5.2 with 256 lanes of
+// one vector or the rows are too few to fill the device otherwise (one row of 8192 f16 3.8 us, 5.2 with 256 lanes of
 // four vectors).
 // ---------------------------------------------------------------------------
 template <int LPR_, int NV_>
@@ -250,7 +250,7 @@ int log2_of(int pow2) { return __builtin_ctz((unsigned)pow2); }
 
 // Lanes of a token: at least one a group and one a slot, and few enough keys a lane.  A round of the
 // choice costs a few steps across the lanes and an operation for each key of a lane, and the
-// tokens of a wave share them: up to 8 keys a lane (16384 tokens of 256 experts, 8 of them: 15.8 us, 19.8
+// tokens of a wave share them: up to 8 keys a lane (16384 tokens of 256 experts, 8 of them: 15.9 us, 19.8
 // with 4 keys), up to 16 where a token would take a whole wave otherwise (32768 of 384, 10 of them: 45
 // us, 50 with 8).
 int token_lanes(int experts, int k, int groups) {
@@ -262,7 +262,7 @@ int token_lanes(int experts, int k, int groups) {
 }
 
 // Slots that a workgroup of the ordering aims at: with fewer, every workgroup has more counts to read (the second
-// kernel of 131072 slots of 256 experts 8.0 us, 9.5 with 1024; 24594 of 60: 5.5 and 5.7).
+// kernel of 131072 slots of 256 experts 7.9 us, 9.5 with 1024; 24594 of 60: 5.7 either way).
 constexpr int64_t kOrderRun = 2048, kOrderMaxBlocks = 256;
 
 struct OrderPlan {
@@ -304,7 +304,7 @@ int check_choice(const char* fn, int dtype, int score, int64_t rows, int experts
 // Distillation.  Threads of a row's workgroup and vectors a thread: in registers while a
 // thread of 1024 needs at most 16, re-read above that (NV = 0).  Short rows take few threads with many
 // vectors each, so that more rows are under way on a compute unit: 8192 rows of 11093 bf16, soft term alone, 72 us with
-// 256 threads of 8 vectors, 110 with 1024 of 2 (the loss alone 36 and 74); 65536 of 2048 f16 112 us with 128 of 2,
+// 256 threads of 8 vectors, 110 with 1024 of 2 (the loss alone 37 and 74); 65536 of 2048 f16 114 us with 128 of 2,
 // 164 with 256 of 1.
 // ---------------------------------------------------------------------------
 template <int NT_, int NV_>
