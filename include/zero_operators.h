@@ -9,6 +9,10 @@
  *                     slots ordered by expert; backward
  *   zero_distill      loss and gradient of a student's logits against a
  *                     teacher's top logits, with a hard-label term
+ *   zero_expert       products of the experts' rows with their weights, the weights'
+ *                     gradient; a token's slots joined; backward
+ *   zero_log_probs    log probabilities of given tokens, entropy and the likeliest
+ *                     tokens of a row (a teacher's list); backward
  *
  * Mixed precision as in ZeRO (Rajbhandari et al., arXiv 1910.02054) Sec. 3.1: the
  * gradient carries the loss scale from the loss on (grad_scale below); where it
@@ -22,7 +26,8 @@
  *     (`workspace`, sized by the function named there) and may use it for anything
  *     else once the call's work on the stream is complete.
  *   - Calls only enqueue kernels on `stream` and can be captured into a graph.
- *     They write all of every output and read no output's old contents.
+ *     They write all of every output (but for rows that a call says it leaves as they
+ *     are) and read no output's old contents.
  *   - `dtype` is the type of a record's arrays declared void* (ZERO_F32,
  *     ZERO_F16, ZERO_BF16).  Arithmetic is in fp32 whatever the type, each output
  *     is rounded once, to nearest even.  A softmax's terms below 2^-126 count as 0, and so
@@ -268,6 +273,178 @@ typedef struct {
 int zero_distill_step(const zero_distill_args_t* args, void* stream);
 int zero_distill_loss(const zero_distill_args_t* args, void* stream);
 int zero_distill_backward(const zero_distill_args_t* args, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Products grouped by expert                                               */
+/* ------------------------------------------------------------------------ */
+
+#define ZERO_EXPERT_MAX_COLS (1 << 20)
+#define ZERO_EXPERT_WORKSPACE_MAX (1 << 24)
+
+/* Rows of the experts' order: row i, for i in [offsets[e], offsets[e+1]), is slot
+ * order[i] and belongs to expert e, as zero_route_order leaves them.  A matrix of rows
+ * lies in one of three ways, which its `*_slots` member names:
+ *   0  in the experts' order: row i
+ *   1  in the slots' order: row order[i]
+ *   n  one row for n slots that follow one another: row order[i] / n.  With n = k
+ *      that is a token's row for each of its k slots.
+ * offsets and order are device arrays that the host does not look at.  Offsets that
+ * fall or leave [0, slots] are taken as the nearest that do not; an entry of order
+ * outside [0, slots) gives a row of zeros where it is read, and none where one is written.
+ *
+ * y's row = x's row times the expert's weights, each sum in fp32:
+ *   y[i][n] = sum over c of x[i][c] * weight[e][c][n]      (transposed: weight[e][n][c])
+ * so the transposed call on the rows' gradients gives the gradient of x; where x's rows
+ * are tokens', zero_expert_mix without weights adds up what their slots got.
+ * Rows of y that belong to no expert are left as they are.  order names no slot twice
+ * where y lies in the slots' order. */
+typedef struct {
+    int32_t dtype;         /* of x, weight and y                                    */
+    int32_t experts;       /* 1 .. ZERO_ROUTE_MAX_EXPERTS                           */
+    int64_t slots;         /* < 2^31                                                */
+    int64_t cols_in, cols_out; /* of x and of y; 1 .. ZERO_EXPERT_MAX_COLS          */
+    int32_t transposed;    /* weight[e] is [cols_out, cols_in], else [cols_in, cols_out] */
+    int32_t x_slots;       /* how x's rows lie; divides slots where it is more than 1 */
+    int32_t y_slots;       /* how y's rows lie: 0 or 1                              */
+    int32_t pad_;
+    const int32_t* offsets; /* [experts + 1]                                        */
+    const int32_t* order;  /* [slots]; NULL where x_slots and y_slots are 0         */
+    const void* x;         /* [slots, cols_in], or [slots / x_slots, cols_in]       */
+    int64_t ld_x;
+    const void* weight;    /* the experts' matrices after one another, all rows ld apart */
+    int64_t ld_weight;
+    void* y;               /* [slots, cols_out]                                     */
+    int64_t ld_y;
+} zero_expert_product_args_t;
+
+int zero_expert_product(const zero_expert_product_args_t* args, void* stream);
+
+/* The gradient of the weights:
+ *   dweight[e][c][n] = sum over the rows i of expert e of x[i][c] * dy[i][n],
+ * 0 for an expert without rows.  (Of weights that lie [cols_out, cols_in]: the same call with x and dy
+ * in each other's place.)  The sum's order is fixed by the sizes and the offsets: the same call gives the same bits. */
+typedef struct {
+    int32_t dtype;         /* of x, dy and dweight                                  */
+    int32_t experts;
+    int64_t slots;
+    int64_t cols_in, cols_out; /* of x and of dy                                    */
+    int32_t x_slots, dy_slots; /* how the rows of x and dy lie                      */
+    const int32_t* offsets;
+    const int32_t* order;  /* NULL where x_slots and dy_slots are 0                 */
+    const void* x;
+    int64_t ld_x;
+    const void* dy;
+    int64_t ld_dy;
+    void* dweight;         /* [experts * cols_in, cols_out]                         */
+    int64_t ld_dweight;
+    float* workspace;      /* zero_expert_workspace(...) floats; NULL if 0          */
+    int64_t workspace_floats;
+} zero_expert_weight_backward_args_t;
+
+int zero_expert_weight_backward(const zero_expert_weight_backward_args_t* args, void* stream);
+
+/* Floats of workspace that zero_expert_weight_backward needs, into *floats (host): at
+ * most ZERO_EXPERT_WORKSPACE_MAX. */
+int zero_expert_workspace(int64_t slots, int32_t experts, int64_t cols_in, int64_t cols_out, int64_t* floats);
+
+/* A token's k slots joined:
+ *   out[t] = base[t] + sum over i of weight[t][i] * y[t * k + i],
+ * in fp32 in that order, over the slots that have an expert: an index below 0, or not below
+ * `experts` where that is not 0, has none, and its row is not looked at. */
+typedef struct {
+    int32_t dtype;         /* of y, base and out                                    */
+    int32_t k;             /* 1 .. ZERO_ROUTE_MAX_K                                 */
+    int64_t tokens, cols;  /* tokens * k < 2^31; 1 <= cols <= ZERO_EXPERT_MAX_COLS  */
+    int32_t experts, pad_; /* 0: no index is too large                              */
+    const int32_t* index;  /* [tokens, k]; NULL: every slot has an expert           */
+    const float* weight;   /* [tokens, k]; NULL: 1                                  */
+    const void* y;         /* [tokens * k, cols], in the slots' order               */
+    int64_t ld_y;
+    const void* base;      /* [tokens, cols]; NULL: none                            */
+    int64_t ld_base;
+    void* out;             /* [tokens, cols]; may be base in place                  */
+    int64_t ld_out;
+} zero_expert_mix_args_t;
+
+int zero_expert_mix(const zero_expert_mix_args_t* args, void* stream);
+
+/* Its gradients (base's is dout):
+ *   dy[t * k + i] = weight[t][i] * dout[t],   dweight[t][i] = dout[t] . y[t * k + i],
+ * both 0 in slots without an expert, whose rows of y are not looked at. */
+typedef struct {
+    int32_t dtype;         /* of dout, y and dy                                     */
+    int32_t k;
+    int64_t tokens, cols;
+    int32_t experts, pad_;
+    const int32_t* index;
+    const float* weight;   /* NULL: 1                                               */
+    const void* dout;      /* [tokens, cols]                                        */
+    int64_t ld_dout;
+    const void* y;         /* [tokens * k, cols]; NULL where dweight is             */
+    int64_t ld_y;
+    void* dy;              /* [tokens * k, cols]; NULL: not wanted; may be y in place */
+    int64_t ld_dy;
+    float* dweight;        /* [tokens, k]; NULL: not wanted                         */
+} zero_expert_mix_backward_args_t;
+
+int zero_expert_mix_backward(const zero_expert_mix_backward_args_t* args, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Log probabilities                                                        */
+/* ------------------------------------------------------------------------ */
+
+#define ZERO_LOG_PROBS_MAX_K 1024
+
+/* With p = softmax of a row's logits / temperature,
+ *   logp    = log p[token], 0 where the token lies outside [0, vocab)
+ *   entropy = - sum over v of p_v log p_v            (nats; p_v = 0 adds nothing)
+ *   top     = the k tokens of the largest logits in falling order, equal ones by the
+ *             lowest token, and their log p.  NaN and -inf logits are not listed; entries
+ *             for which no token is left have index -1 and log probability -inf.
+ *             zero_distill_* takes such lists (teacher_dtype ZERO_F32) as they are.
+ * A row of nothing but -inf has log probability -inf, entropy 0 and an empty list; with a
+ * NaN or +inf in the row, log probabilities and entropy are NaN.
+ * stats, for the backward: the largest logit, the sum of exp((z - largest) / temperature), the
+ * entropy. */
+typedef struct {
+    int32_t dtype;         /* of logits                                             */
+    int32_t k;             /* entries a row, 0 <= k <= ZERO_LOG_PROBS_MAX_K         */
+    int64_t rows, vocab;   /* vocab in [1, 2^30]                                    */
+    double temperature;    /* in [1e-30, 1e30]                                      */
+    const void* logits;    /* [rows, vocab]                                         */
+    int64_t ld_logits;
+    const int32_t* tokens; /* [rows]; NULL where logp is                            */
+    float* logp;           /* [rows]; NULL: not wanted                              */
+    float* entropy;        /* [rows]; NULL: not wanted                              */
+    int32_t* top_index;    /* [rows, k]; NULL if k = 0                              */
+    float* top_logp;       /* [rows, k]; NULL if k = 0                              */
+    float* stats;          /* [rows, 3]; NULL: not wanted                           */
+} zero_log_probs_args_t;
+
+int zero_log_probs(const zero_log_probs_args_t* args, void* stream);
+
+/* The gradient of the logits from those of logp and entropy:
+ *   dlogits_v = grad_scale / temperature * ( dlogp * ([v = token] - p_v)
+ *                                            - dentropy * p_v * (log p_v + entropy) ),
+ * the first term where the token lies in [0, vocab); p_v = 0 has no part in the second.  (The
+ * lists have no gradient.)  A row of nothing but -inf has gradient 0.  */
+typedef struct {
+    int32_t dtype;         /* of logits and dlogits                                 */
+    int32_t pad_;
+    int64_t rows, vocab;
+    double temperature;
+    double grad_scale;     /* finite in fp32; the loss scale                        */
+    const void* logits;
+    int64_t ld_logits;
+    const int32_t* tokens; /* NULL where dlogp is                                   */
+    const float* stats;    /* of zero_log_probs at this temperature                 */
+    const float* dlogp;    /* [rows]; NULL: 0                                       */
+    const float* dentropy; /* [rows]; NULL: 0                                       */
+    void* dlogits;         /* [rows, vocab]; may be logits in place                 */
+    int64_t ld_dlogits;
+} zero_log_probs_backward_args_t;
+
+int zero_log_probs_backward(const zero_log_probs_backward_args_t* args, void* stream);
 
 #ifdef __cplusplus
 }

@@ -108,25 +108,6 @@ enum DistillKind {
     kTwoSums,  // an exponential for each
 };
 
-// This thread's maximum of PER packed values.
-template <typename T>
-__device__ __forceinline__ float max_of(u32x4 v, float m) {
-    if constexpr (T::kLowest == F16::kLowest) {
-        typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-        const f16x8 h = __builtin_bit_cast(f16x8, v);
-        const auto a = __builtin_elementwise_max(h.lo, h.hi);
-        const auto b = __builtin_elementwise_max(a.lo, a.hi);
-        return fmaxf(fmaxf(m, (float)b.x), (float)b.y);
-    } else {
-        float f[T::kPer];
-        T::unpack(v, f);
-#pragma unroll
-        for (int j = 0; j < T::kPer; ++j)
-            m = fmaxf(m, f[j]);
-        return m;
-    }
-}
-
 template <typename T, int KIND>
 __device__ __forceinline__ void add_term(float f, const Against<T>& x, const Against<T>& x1, float& s, float& s1) {
     const float e = exp2_fast(x(f));

@@ -1,5 +1,5 @@
-// row_ops.hpp -- what the row operators' kernels share (norm_kernels.hpp,
-// route_kernels.hpp, distill_kernels.hpp): 16-byte vectors of the three element types at any
+// row_ops.hpp -- what the row operators' kernels share (norm_kernels.hpp, route_kernels.hpp,
+// distill_kernels.hpp, expert_kernels.hpp, log_prob_kernels.hpp): 16-byte vectors of the three element types at any
 // element alignment, and reductions over segments of a wave and over a workgroup
 // in the vector ALU.
 //
@@ -180,6 +180,25 @@ struct Cut {
     }
     __device__ __forceinline__ int edge_column(int e) const { return e < head ? e : tail + e - head; }
 };
+
+// The maximum of m and a packed vector's values; a NaN loses.
+template <typename T>
+__device__ __forceinline__ float max_of(u32x4 v, float m) {
+    if constexpr (T::kLowest == F16::kLowest) {
+        typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+        const f16x8 h = __builtin_bit_cast(f16x8, v);
+        const auto a = __builtin_elementwise_max(h.lo, h.hi);
+        const auto b = __builtin_elementwise_max(a.lo, a.hi);
+        return fmaxf(fmaxf(m, (float)b.x), (float)b.y);
+    } else {
+        float f[T::kPer];
+        T::unpack(v, f);
+#pragma unroll
+        for (int j = 0; j < T::kPer; ++j)
+            m = fmaxf(m, f[j]);
+        return m;
+    }
+}
 
 // Keeps a packed vector in its registers between two passes over it: without it the compiler holds
 // the first pass's fp32 values for the second, at twice the registers or more.

@@ -31,15 +31,23 @@ ROUTE_ARGS = struct.Struct("@iiqiiiiiidPqPPP")
 ROUTE_ORDER_ARGS = struct.Struct("@PqiiPPPq")
 ROUTE_BACKWARD_ARGS = struct.Struct("@iiqiiiidPqPPPPq")
 DISTILL_ARGS = struct.Struct("@iiqqiiddddPqPPPPPPPPq")
+EXPERT_PRODUCT_ARGS = struct.Struct("@iiqqqiiiiPPPqPqPq")
+EXPERT_WEIGHT_BACKWARD_ARGS = struct.Struct("@iiqqqiiPPPqPqPqPq")
+EXPERT_MIX_ARGS = struct.Struct("@iiqqiiPPPqPqPq")
+EXPERT_MIX_BACKWARD_ARGS = struct.Struct("@iiqqiiPPPqPqPqP")
+LOG_PROBS_ARGS = struct.Struct("@iiqqdPqPPPPPP")
+LOG_PROBS_BACKWARD_ARGS = struct.Struct("@iiqqddPqPPPPPq")
 
 EXPORTS = ("zero_rms_norm", "zero_rms_norm_backward", "zero_rms_norm_workspace", "zero_route", "zero_route_order",
            "zero_route_workspace", "zero_route_backward", "zero_distill_step", "zero_distill_loss",
-           "zero_distill_backward")
+           "zero_distill_backward", "zero_expert_product", "zero_expert_weight_backward", "zero_expert_workspace",
+           "zero_expert_mix", "zero_expert_mix_backward", "zero_log_probs", "zero_log_probs_backward")
 for _f in EXPORTS:
     getattr(_lib, _f).restype = ctypes.c_int
     getattr(_lib, _f).argtypes = [_P, _P]
 _lib.zero_rms_norm_workspace.argtypes = [_i64, _i64, ctypes.POINTER(_i64)]
 _lib.zero_route_workspace.argtypes = [_i64, _i32, ctypes.POINTER(_i64)]
+_lib.zero_expert_workspace.argtypes = [_i64, _i32, _i64, _i64, ctypes.POINTER(_i64)]
 
 
 _raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
@@ -293,3 +301,139 @@ def zero_distill_backward(logits, teacher_index, teacher_logits, stats, dlogits,
     dloss (float32, [rows]; None: 1)."""
     _distill(_lib.zero_distill_backward, logits, teacher_index, teacher_logits, None, stats, dlogits, dloss, labels,
              soft, hard, temperature, row_weight, grad_scale, stream)
+
+
+def _rows_of(slots, per):
+    return slots // per if per > 1 else slots
+
+
+def zero_expert_product(x, weight, offsets, y, order=None, x_slots=0, y_slots=0, transposed=False, stream=None):
+    """Each row of x times its expert's weights, into y [slots, cols_out].  offsets [experts + 1] and order [slots] are
+    zero_route_order's; weight [experts, cols_in, cols_out], or [experts, cols_out, cols_in] with `transposed`.  x_slots
+    0: x's rows lie in the experts' order; 1: in the slots'; n: slot s has row s // n (n = k: tokens' rows).  y_slots
+    0 or 1 likewise.  The transposed call on the rows' gradient gives x's.  Rows of y that belong to no expert
+    stay as they are."""
+    code, dt = _type(x, "x"), x.dtype
+    dev = x.get_device()
+    cols_in, (slots, cols_out) = _sizes(x, "x")[1], _sizes(y, "y")
+    experts = offsets.numel() - 1
+    px, ld_x = _matrix(x, dt, "x", (_rows_of(slots, x_slots), cols_in), dev)
+    size = (experts * cols_out, cols_in) if transposed else (experts * cols_in, cols_out)
+    pw, ld_w = _matrix(weight, dt, "weight", size, dev)
+    py, ld_y = _matrix(y, dt, "y", (slots, cols_out), dev)
+    args = EXPERT_PRODUCT_ARGS.pack(code, experts, slots, cols_in, cols_out, bool(transposed), x_slots, y_slots, 0,
+                                    _vector(offsets, _I32, "offsets", experts + 1, dev),
+                                    _vector(order, _I32, "order", slots, dev), px, ld_x, pw, ld_w, py, ld_y)
+    rc = _lib.zero_expert_product(args, _on(stream, dev))
+    if rc < 0:
+        _check(rc)
+
+
+def zero_expert_workspace(slots, experts, cols_in, cols_out):
+    """Floats of workspace that zero_expert_weight_backward needs for these sizes (at most 2^24)."""
+    out = _i64()
+    _check(_lib.zero_expert_workspace(int(slots), int(experts), int(cols_in), int(cols_out), ctypes.byref(out)))
+    return out.value
+
+
+def zero_expert_weight_backward(x, dy, offsets, dweight, workspace=None, order=None, x_slots=0, dy_slots=0,
+                                stream=None):
+    """The gradient of zero_expert_product's weights, dweight [experts, cols_in, cols_out], from its x and y's gradient
+    dy, whose rows lie as x_slots and dy_slots say.  (Of transposed weights: x and dy in each other's place.)
+    workspace: a float32 tensor of at least zero_expert_workspace(slots, experts, cols_in, cols_out) elements."""
+    code, dt = _type(x, "x"), x.dtype
+    dev = x.get_device()
+    cols_in, (dy_rows, cols_out) = _sizes(x, "x")[1], _sizes(dy, "dy")
+    experts = offsets.numel() - 1
+    slots = order.numel() if order is not None else dy_rows
+    px, ld_x = _matrix(x, dt, "x", (_rows_of(slots, x_slots), cols_in), dev)
+    pdy, ld_dy = _matrix(dy, dt, "dy", (_rows_of(slots, dy_slots), cols_out), dev)
+    pdw, ld_dw = _matrix(dweight, dt, "dweight", (experts * cols_in, cols_out), dev)
+    pw, n = _room(workspace, _F32, "workspace", dev)
+    args = EXPERT_WEIGHT_BACKWARD_ARGS.pack(code, experts, slots, cols_in, cols_out, x_slots, dy_slots,
+                                            _vector(offsets, _I32, "offsets", experts + 1, dev),
+                                            _vector(order, _I32, "order", slots, dev), px, ld_x, pdy, ld_dy, pdw,
+                                            ld_dw, pw, n)
+    rc = _lib.zero_expert_weight_backward(args, _on(stream, dev))
+    if rc < 0:
+        _check(rc)
+
+
+def zero_expert_mix(y, index, out, weight=None, base=None, experts=0, stream=None):
+    """out[t] = base[t] + sum over i of weight[t][i] * y[t * k + i], over the slots with an expert: index (int32,
+    [tokens, k]) not below 0 and, where experts is not 0, below it.  y [tokens * k, cols]; weight float32 [tokens, k]
+    (None: 1); base like out (None: 0), which may be base in place."""
+    code, dt = _type(out, "out"), out.dtype
+    dev = out.get_device()
+    size = tokens, cols = _sizes(out, "out")
+    k = index.shape[-1]
+    po, ld_o = _matrix(out, dt, "out", size, dev)
+    py, ld_y = _matrix(y, dt, "y", (tokens * k, cols), dev)
+    pb, ld_b = _matrix(base, dt, "base", size, dev)
+    args = EXPERT_MIX_ARGS.pack(code, k, tokens, cols, experts, 0, _vector(index, _I32, "index", tokens * k, dev),
+                                _vector(weight, _F32, "weight", tokens * k, dev), py, ld_y, pb, ld_b, po, ld_o)
+    rc = _lib.zero_expert_mix(args, _on(stream, dev))
+    if rc < 0:
+        _check(rc)
+
+
+def zero_expert_mix_backward(dout, y, index, weight, dy, dweight=None, experts=0, stream=None):
+    """The gradients of zero_expert_mix from dout [tokens, cols]: dy [tokens * k, cols] (may be y in place; None: not
+    wanted) and dweight [tokens, k] float32 (None: not wanted, then y is None too); both 0 in slots without an
+    expert.  base's gradient is dout."""
+    code, dt = _type(dout, "dout"), dout.dtype
+    dev = dout.get_device()
+    size = tokens, cols = _sizes(dout, "dout")
+    k = index.shape[-1]
+    pd, ld_d = _matrix(dout, dt, "dout", size, dev)
+    py, ld_y = _matrix(y, dt, "y", (tokens * k, cols), dev)
+    pdy, ld_dy = _matrix(dy, dt, "dy", (tokens * k, cols), dev)
+    args = EXPERT_MIX_BACKWARD_ARGS.pack(code, k, tokens, cols, experts, 0,
+                                         _vector(index, _I32, "index", tokens * k, dev),
+                                         _vector(weight, _F32, "weight", tokens * k, dev), pd, ld_d, py, ld_y, pdy,
+                                         ld_dy, _vector(dweight, _F32, "dweight", tokens * k, dev))
+    rc = _lib.zero_expert_mix_backward(args, _on(stream, dev))
+    if rc < 0:
+        _check(rc)
+
+
+def zero_log_probs(logits, tokens, logp, entropy=None, top_index=None, top_logp=None, temperature=1.0, stats=None,
+                   stream=None):
+    """With p = softmax(logits / temperature) of each row of logits [rows, vocab]: logp = log p[tokens] (float32,
+    [rows]; tokens int32, outside the vocabulary: 0; both may be None), entropy (float32, [rows]) in nats, and the k
+    likeliest tokens top_index (int32) and their log p top_logp (float32), both [rows, k], in falling order, equal
+    ones by the lowest token: a list for zero_distill_*.  stats (float32, [rows, 3]) is what
+    zero_log_probs_backward needs."""
+    code, dt = _type(logits, "logits"), logits.dtype
+    dev = logits.get_device()
+    size = rows, vocab = _sizes(logits, "logits")
+    pl, ld = _matrix(logits, dt, "logits", size, dev)
+    k = 0 if top_index is None else top_index.shape[-1]
+    args = LOG_PROBS_ARGS.pack(code, k, rows, vocab, temperature, pl, ld, _vector(tokens, _I32, "tokens", rows, dev),
+                               _vector(logp, _F32, "logp", rows, dev), _vector(entropy, _F32, "entropy", rows, dev),
+                               _vector(top_index, _I32, "top_index", rows * k, dev),
+                               _vector(top_logp, _F32, "top_logp", rows * k, dev),
+                               _vector(stats, _F32, "stats", 3 * rows, dev))
+    rc = _lib.zero_log_probs(args, _on(stream, dev))
+    if rc < 0:
+        _check(rc)
+
+
+def zero_log_probs_backward(logits, tokens, stats, dlogits, dlogp=None, dentropy=None, temperature=1.0, grad_scale=1.0,
+                            stream=None):
+    """The gradient of the logits into dlogits (like logits; may be logits in place) from zero_log_probs's stats at the
+    same temperature and the gradients of its log probabilities and entropies (float32, [rows]; None: 0; tokens may be
+    None where dlogp is).  grad_scale is the loss scale.  The lists have no gradient."""
+    code, dt = _type(logits, "logits"), logits.dtype
+    dev = logits.get_device()
+    size = rows, vocab = _sizes(logits, "logits")
+    pl, ld = _matrix(logits, dt, "logits", size, dev)
+    pd, ld_d = _matrix(dlogits, dt, "dlogits", size, dev)
+    args = LOG_PROBS_BACKWARD_ARGS.pack(code, 0, rows, vocab, temperature, grad_scale, pl, ld,
+                                        _vector(tokens, _I32, "tokens", rows, dev) if dlogp is not None else 0,
+                                        _vector(stats, _F32, "stats", 3 * rows, dev),
+                                        _vector(dlogp, _F32, "dlogp", rows, dev),
+                                        _vector(dentropy, _F32, "dentropy", rows, dev), pd, ld_d)
+    rc = _lib.zero_log_probs_backward(args, _on(stream, dev))
+    if rc < 0:
+        _check(rc)
