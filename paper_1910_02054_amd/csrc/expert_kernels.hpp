@@ -15,6 +15,8 @@
 // a lane then holds neighbouring columns of one row of the result.
 #pragma once
 
+#include <type_traits>
+
 #include "row_ops.hpp"
 #include "zero_operators.h"
 
@@ -183,10 +185,14 @@ __device__ __forceinline__ void multiply(const char* stage, const XS& xs, const 
     }
 }
 
-// 16 bytes straight to LDS: lane l's land at base + 16 l.
-__device__ __forceinline__ void copy_to_lds(const void* from, char* base) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, ZO_LDS(void, base), 16, 0, 0);
+// 16 bytes straight to LDS: lane l's land at base + 16 l.  Written as an instruction because the compiler holds every
+// ds_read_tr behind all copies that it knows of (s_waitcnt vmcnt(0) before the step's first fragment: 16384 x 8 slots
+// 1024 to 4096 bf16 1612 us); wait_stage has the waits.  There is no output register, and nothing else in these kernels uses m0.
+__device__ __forceinline__ void copy_to_lds(const void* from, uint32_t base) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(base), "v"(from) : "memory");
 }
+
+__device__ __forceinline__ uint32_t lds_address(char* p) { return (uint32_t)(uintptr_t)ZO_LDS(char, p); }
 
 // Until at most LEFT of this wave's loads are under way, and all waves have come here: with 0 (or the loads of the
 // later stages) left, a stage's copies have landed, and what was read from the stage to be filled next has been.
@@ -355,61 +361,70 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall
     const elem* px[S::kRowLoads];
     const elem* pw[S::kColLoads];
     int wc[S::kColLoads];
-    const int xr = t / 8, xc = (t & 7) ^ along_exchange<false>(xr);
+    const int xr = t / 8, xc = ((t & 7) ^ along_exchange<false>(xr)) * kPer;
 #pragma unroll
     for (int j = 0; j < S::kRowLoads; ++j) {  // rows past the run's are not stored
         const uint32_t i = (uint32_t)place.first + xr + j * kXRows;  // may pass 2^31
         const int64_t row = row_at(a.order, a.x_map, a.slots, i < (uint32_t)place.end ? i : place.end - 1);
-        px[j] = row < 0 ? nullptr : x + row * a.ld_x;
+        px[j] = x + (row < 0 ? 0 : row) * a.ld_x;  // none: stored as zeros
+        if constexpr (DMA)
+            px[j] += xc;
     }
 #pragma unroll
     for (int j = 0; j < S::kColLoads; ++j) {
         const int r = t / kChunks + j * kWRows;
         if constexpr (ALONG) {
-            wc[j] = (t & 7) ^ along_exchange<true>(r);
+            wc[j] = ((t & 7) ^ along_exchange<true>(r)) * kPer;
             const int n = n0 + r < a.cols_out ? n0 + r : a.cols_out - 1;  // columns past the last are not stored
             pw[j] = w + n * a.ld_w;
+            if constexpr (DMA)
+                pw[j] += wc[j];
         } else {
-            wc[j] = (t % kChunks) ^ across_exchange<T, kChunks>(r);
+            wc[j] = n0 + ((t % kChunks) ^ across_exchange<T, kChunks>(r)) * kPer;
             pw[j] = w + r * a.ld_w;
-            if constexpr (DMA) {
-                const int col = n0 + wc[j] * kPer;
-                pw[j] += col < a.cols_out ? col : a.cols_out - kPer;
-            }
+            if constexpr (DMA)
+                pw[j] += wc[j] < a.cols_out ? wc[j] : a.cols_out - kPer;
         }
     }
+    const int64_t w_step = ALONG ? 1 : a.ld_w;  // elements of the weights for a place of the axis
+    const uint32_t lds = lds_address(tiles) + wave * 1024;
     u32x4 rx[DMA ? 1 : S::kRowLoads], rw[DMA ? 1 : S::kColLoads];
 
+    // WHOLE: the step lies before the end of the axis
+    auto copy = [&](int step, auto whole) __attribute__((always_inline)) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        const int k0 = step * kStep;
+        const uint32_t stage = lds + step % S::kStages * S::kStage;
+#pragma unroll
+        for (int j = 0; j < S::kRowLoads; ++j)
+            copy_to_lds(WHOLE || k0 + xc < depth ? px[j] + k0 : zeros, stage + j * S::kThreads * 16);
+#pragma unroll
+        for (int j = 0; j < S::kColLoads; ++j) {
+            const int place_of = ALONG ? wc[j] : t / kChunks + j * kWRows;
+            copy_to_lds(WHOLE || k0 + place_of < depth ? pw[j] + k0 * w_step : zeros,
+                        stage + S::kRowsBytes + j * S::kThreads * 16);
+        }
+    };
     auto fetch = [&](int step) __attribute__((always_inline)) {
         const int k0 = step * kStep;
         if constexpr (DMA) {
-            char* const stage = tiles + step % S::kStages * S::kStage + wave * 1024;
-            const bool x_there = k0 + xc * kPer < depth;
-#pragma unroll
-            for (int j = 0; j < S::kRowLoads; ++j)
-                copy_to_lds(x_there && px[j] ? px[j] + k0 + xc * kPer : zeros, stage + j * S::kThreads * 16);
-#pragma unroll
-            for (int j = 0; j < S::kColLoads; ++j) {
-                const elem* from;
-                if constexpr (ALONG)
-                    from = k0 + wc[j] * kPer < depth ? pw[j] + k0 + wc[j] * kPer : zeros;
-                else
-                    from = k0 + t / kChunks + j * kWRows < depth ? pw[j] + k0 * a.ld_w : zeros;
-                copy_to_lds(from, stage + S::kRowsBytes + j * S::kThreads * 16);
-            }
+            if (k0 + kStep <= depth)
+                copy(step, std::true_type());
+            else
+                copy(step, std::false_type());
         } else {
-            const u32x4 none = {0, 0, 0, 0};
 #pragma unroll
             for (int j = 0; j < S::kRowLoads; ++j)
-                rx[j] = px[j] ? load_row<T>(px[j], k0 + xc * kPer, depth, 0) : none;
+                rx[j] = load_row<T>(px[j], k0 + xc, depth, 0);
 #pragma unroll
             for (int j = 0; j < S::kColLoads; ++j) {
-                if constexpr (ALONG)
-                    rw[j] = load_row<T>(pw[j], k0 + wc[j] * kPer, depth, 0);
-                else
-                    rw[j] = k0 + t / kChunks + j * kWRows < depth
-                                ? load_row<T>(pw[j] + k0 * a.ld_w, n0 + wc[j] * kPer, a.cols_out, 0)
-                                : none;
+                if constexpr (ALONG) {
+                    rw[j] = load_row<T>(pw[j], k0 + wc[j], depth, 0);
+                } else {
+                    rw[j] = u32x4{0, 0, 0, 0};
+                    if (k0 + t / kChunks + j * kWRows < depth)
+                        rw[j] = load_row<T>(pw[j] + k0 * w_step, wc[j], a.cols_out, 0);
+                }
             }
         }
     };
@@ -455,6 +470,16 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall
             put(s + kAhead);
     }
 
+    if (a.x_map.mode && !a.out_map.mode) {  // rows without a slot; in the slots' order they are not stored
+#pragma unroll
+        for (int m = 0; m < S::kTm; ++m) {
+            const uint32_t i = (uint32_t)place.first + (wm * S::kTm + m) * 16 + (lane & 15);
+            if (row_at(a.order, a.x_map, a.slots, i < (uint32_t)place.end ? i : place.end - 1) < 0)
+#pragma unroll
+                for (int n = 0; n < S::kTn; ++n)
+                    acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
     elem* const y = static_cast<elem*>(a.out);
     store_tile<T, S, ALONG>(acc, n0 + wn * S::kTn * 16, a.cols_out, lane, [&](int m) -> elem* {
         const uint32_t i = (uint32_t)place.first + wm * S::kTm * 16 + m;
@@ -510,6 +535,7 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_weight_back(const Expert
             wc[j] = wc[j] < a.cols_out ? wc[j] : a.cols_out - kPer;
         }
     }
+    const uint32_t lds = lds_address(tiles) + wave * 1024;
     const bool ordered = a.x_map.mode | a.out_map.mode;
     // entries of order for a step's rows, a step before they are needed; -1: no row
     int32_t slot[kLoads];
@@ -522,7 +548,7 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_weight_back(const Expert
     };
     u32x4 rx[DMA ? 1 : kLoads], rw[DMA ? 1 : kLoads];
     auto fetch = [&](int step) __attribute__((always_inline)) {
-        char* const stage = tiles + (step & 1) * S::kStage + wave * 1024;
+        const uint32_t stage = lds + (step & 1) * S::kStage;
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             const int64_t i = begin + (int64_t)step * kStep + t / kChunks + j * kRows;
