@@ -1,9 +1,9 @@
 // expert_kernels.hpp -- products of the experts' rows with their weights, and the weights'
 // gradient: tiles of both operands in LDS, sums in the matrix cores' registers.
 //
-// A step of the sum takes 128 bytes of its axis (64 elements of 16 bits, 32 of fp32).  An operand's tile
+// A step of the sum takes 64 or 128 bytes of its axis (32 or 64 elements of 16 bits).  An operand's tile
 // comes in one of two layouts, as it lies in memory:
-//   along    its rows run along the summed axis (x; weights that lie [out, in]): tile rows of 128 bytes
+//   along    its rows run along the summed axis (x; weights that lie [out, in]): tile rows of a step's bytes
 //   across   they run across it (weights that lie [in, out]; both operands of the gradient): one
 //            tile row for each place of the axis, which the matrix instruction wants transposed;
 //            ds_read_b64_tr_b16 does that for 16 bits, fp32's fragments are single words anyway
@@ -29,8 +29,6 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef u32x2 u32x2_e2 __attribute__((aligned(2)));
-
-constexpr int kStepBytes = 128;  // of the summed axis
 
 // The rows of a matrix (ZERO's `*_slots`): `mode` 0, 1 or n; a slot's row for n is slot * mul >> shift.
 struct SlotMap {
@@ -91,11 +89,14 @@ __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
     }
 }
 
-// Along: the exchange of the chunks of tile row r.  On the columns' side a pair of fragments takes 32 rows so that a lane's
-// 4 + 4 results are neighbours: fragment f, lane row a is tile row 32 (f / 2) + 8 (a / 4) + 4 (f % 2) + a % 4.
-template <bool PAIRED>
+// Along: the exchange of the chunks of tile row r, rows of BYTES.  On the columns' side a pair of fragments takes 32 rows so
+// that a lane's 4 + 4 results are neighbours: fragment f, lane row a is tile row 32 (f / 2) + 8 (a / 4) + 4 (f % 2) + a % 4.
+template <bool PAIRED, int BYTES>
 __device__ __forceinline__ int along_exchange(int r) {
-    return PAIRED ? (r & 3) | (r >> 3 & 1) << 2 : r & 7;
+    if constexpr (BYTES == 128)
+        return PAIRED ? (r & 3) | (r >> 3 & 1) << 2 : r & 7;
+    else
+        return (r >> (PAIRED ? 4 : 3) & 1) * 3;
 }
 
 // Across: the exchange of the chunks of the tile row of place k, for rows of CHUNKS chunks.
@@ -107,20 +108,22 @@ __device__ __forceinline__ int across_exchange(int k) {
         return (((k & 3) | (k >> 3 & 1) << 2) << 1) & (CHUNKS - 1);
 }
 
-// One side of a wave's fragments: byte offsets in the tile, once for each fragment or few.
-template <typename T, bool ALONG, bool PAIRED, int TILE, int COUNT>
+// One side of a wave's fragments: byte offsets in the tile, once for each fragment or half step.
+template <typename T, bool ALONG, bool PAIRED, int TILE, int COUNT, int BYTES>
 struct Side {
-    static constexpr int kRow = ALONG ? kStepBytes : TILE * (int)sizeof(typename T::elem);  // bytes of a tile row
+    static constexpr int kRow = ALONG ? BYTES : TILE * (int)sizeof(typename T::elem);  // bytes of a tile row
     static constexpr int kChunks = kRow / 16;
-    int at[ALONG ? 2 : COUNT];
+    static constexpr int kReads = ALONG ? 1 : T::kPer == 4 ? 4 : 2;  // of a fragment
+    int at[ALONG ? BYTES / 64 : COUNT];
     // first: the wave's first row (along) or column (across) in the tile
     __device__ __forceinline__ Side(int first, int lane) {
         const int a = lane & 15, g = lane >> 4;
         if constexpr (ALONG) {
             const int r = first + (PAIRED ? 8 * (a >> 2) + (a & 3) : a);
-            const int c = g ^ along_exchange<PAIRED>(r);
-            at[0] = r * kRow + c * 16;
-            at[1] = r * kRow + (c ^ 4) * 16;
+            const int c = g ^ along_exchange<PAIRED, BYTES>(r);
+#pragma unroll
+            for (int kk = 0; kk < BYTES / 64; ++kk)
+                at[kk] = r * kRow + (c ^ 4 * kk) * 16;
         } else if constexpr (T::kPer == 4) {
 #pragma unroll
             for (int f = 0; f < COUNT; ++f) {
@@ -156,12 +159,14 @@ struct Side {
     }
 };
 
-template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
+// BYTES of the summed axis a step.
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_, int BYTES_>
 struct TileShape {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kStages = STAGES_;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kStages = STAGES_, kBytes = BYTES_;
     static constexpr int kThreads = 64 * WM * WN, kTm = BM / WM / 16, kTn = BN / WN / 16;
-    static constexpr int kRowsBytes = BM * kStepBytes, kColsBytes = BN * kStepBytes, kStage = kRowsBytes + kColsBytes;
+    static constexpr int kRowsBytes = BM * kBytes, kColsBytes = BN * kBytes, kStage = kRowsBytes + kColsBytes;
     static constexpr int kRowLoads = kRowsBytes / 16 / kThreads, kColLoads = kColsBytes / 16 / kThreads;  // a thread's
+    static constexpr int kCopies = kRowLoads + kColLoads;
     static_assert(kRowLoads * 16 * kThreads == kRowsBytes && kColLoads * 16 * kThreads == kColsBytes, "whole loads");
 };
 
@@ -169,7 +174,7 @@ struct TileShape {
 template <typename T, typename S, typename XS, typename WS>
 __device__ __forceinline__ void multiply(const char* stage, const XS& xs, const WS& ws, f32x4 (&acc)[S::kTm][S::kTn]) {
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
+    for (int kk = 0; kk < S::kBytes / 64; ++kk) {
         u32x4 xf[S::kTm], wf[S::kTn];
 #pragma unroll
         for (int n = 0; n < S::kTn; ++n)
@@ -192,7 +197,12 @@ __device__ __forceinline__ void copy_to_lds(const void* from, uint32_t base) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(base), "v"(from) : "memory");
 }
 
-__device__ __forceinline__ uint32_t lds_address(char* p) { return (uint32_t)(uintptr_t)ZO_LDS(char, p); }
+// 4 bytes, lane l's to base + 4 l.
+__device__ __forceinline__ void copy_word_to_lds(const void* from, uint32_t base) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(base), "v"(from) : "memory");
+}
+
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)ZO_LDS(const void, p); }
 
 // Until at most LEFT of this wave's loads are under way, and all waves have come here: with 0 (or the loads of the
 // later stages) left, a stage's copies have landed, and what was read from the stage to be filled next has been.
@@ -205,54 +215,182 @@ __device__ __forceinline__ void wait_stage() {
     asm volatile("" ::: "memory");
 }
 
-// Four neighbouring results of a row (or eight), of which those before column `cols` exist.
-template <typename T, int COUNT>
-__device__ __forceinline__ void store_results(typename T::elem* p, int col, int cols, const float* f) {
-    if (col + COUNT <= cols) {
-        if constexpr (T::kPer == 4) {
+// The tiles that a workgroup takes, one after another, as one run of steps: the copies of a tile's first steps are under way
+// before the tile before it has ended, and its results are stored while they land.
+//   next_step()          prepares the copies of the run's next step; false: there is none
+//   copy(i, stage)       issues copy i of that step, into the stage at LDS address `stage`
+//   tile_steps()         the steps of the next tile, below 0: none
+//   finish(acc)          stores a tile's results
+// A step is two halves of kTm groups of products, one of the rows' fragments with all of the columns'.  Fragments are read
+// kLead groups before they are needed, so kLead groups before a step's end its stage is free for the copies of step s + kStages:
+// there all waves meet, and step s + 1 has landed.
+template <typename T, typename S, typename XS, typename WS, typename NEXT, typename COPY, typename STEPS, typename FINISH>
+__device__ __forceinline__ void multiply_tiles(const char* tiles, uint32_t lds, const XS& xs, const WS& ws, NEXT next_step,
+                                               COPY copy, STEPS tile_steps, FINISH finish) {
+    constexpr int kLead = S::kTm / 2, kHalves = S::kBytes / 64, kGroups = kHalves * S::kTm;
+    static_assert(S::kTm % 2 == 0 && S::kTn % kLead == 0, "whole fragments a group");
+    constexpr int kReads = S::kTn / kLead, kCopyRate = (S::kCopies + kLead - 1) / kLead;
+    bool more = false;
 #pragma unroll
-            for (int j = 0; j < COUNT; j += 4)
-                store_vec<T, false>(p + col + j, T::pack(f + j));
-        } else if constexpr (COUNT == 8) {
+    for (int s = 0; s < S::kStages; ++s) {
+        more = next_step();
+        if (more)
+#pragma unroll
+            for (int i = 0; i < S::kCopies; ++i)
+                copy(i, lds + s * S::kStage);
+    }
+    if (more)
+        wait_stage<(S::kStages - 1) * S::kCopies>();
+    else
+        wait_stage<0>();
+    u32x4 xf[S::kTm], wf[S::kTn], wn[S::kTn];
+#pragma unroll
+    for (int n = 0; n < S::kTn; ++n)
+        wf[n] = ws.load(tiles + S::kRowsBytes, n, 0);
+#pragma unroll
+    for (int m = 0; m < kLead; ++m)
+        xf[m] = xs.load(tiles, m, 0);
+    int at = 0;  // the stage of the step
+    for (int steps; (steps = tile_steps()) >= 0;) {
+        f32x4 acc[S::kTm][S::kTn];
+#pragma unroll
+        for (int m = 0; m < S::kTm; ++m)
+#pragma unroll
+            for (int n = 0; n < S::kTn; ++n)
+                acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < steps; ++s) {
+            const char* from = tiles + at * S::kStage;
+            const uint32_t stage = lds + at * S::kStage;
+#pragma unroll
+            for (int q = 0; q < kGroups; ++q) {
+                const int m = q % S::kTm, ahead = (q + kLead) % kGroups;
+                if (q == kGroups - kLead) {
+                    // in the order of the loads: later ones that are under way can only make the wait longer
+                    if (more)
+                        wait_stage<(S::kStages - 2) * S::kCopies>();
+                    else
+                        wait_stage<0>();
+                    at = at + 1 == S::kStages ? 0 : at + 1;
+                    from = tiles + at * S::kStage;
+                    more = more && next_step();
+                }
+                xf[ahead % S::kTm] = xs.load(from, ahead % S::kTm, ahead / S::kTm);
+                if (m >= kLead)
+#pragma unroll
+                    for (int i = 0; i < kReads; ++i)
+                        wn[(m - kLead) * kReads + i] =
+                            ws.load(from + S::kRowsBytes, (m - kLead) * kReads + i, ahead / S::kTm);
+                if (q >= kGroups - kLead && more)
+#pragma unroll
+                    for (int i = (m - kLead) * kCopyRate; i < (m - kLead + 1) * kCopyRate && i < S::kCopies; ++i)
+                        copy(i, stage);
+#pragma unroll
+                for (int n = 0; n < S::kTn; ++n)
+                    acc[m][n] = mma<T>(wf[n], xf[m], acc[m][n]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (m == S::kTm - 1)
+#pragma unroll
+                    for (int n = 0; n < S::kTn; ++n)
+                        wf[n] = wn[n];
+            }
+        }
+        finish(acc);
+    }
+}
+
+// Four neighbouring results of a row, of which those before column `cols` exist.
+template <typename T>
+__device__ __forceinline__ void store_results(typename T::elem* p, int col, int cols, const float* f) {
+    if (col + 4 <= cols) {
+        if constexpr (T::kPer == 4) {
             store_vec<T, false>(p + col, T::pack(f));
         } else {
-            float g[8];
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                g[j] = g[j + 4] = f[j];
+            const float g[8] = {f[0], f[1], f[2], f[3], f[0], f[1], f[2], f[3]};
             const u32x4 v = T::pack(g);
             *reinterpret_cast<u32x2_e2*>(p + col) = u32x2{v.x, v.y};
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < COUNT; ++j)
+        for (int j = 0; j < 4; ++j)
             if (col + j < cols)
                 p[col + j] = T::of_f32(f[j]);
     }
 }
 
-// A wave's results: out(m) is the row of its m-th (null: none), `first` its first column.
+// A lane's value of the lane eight away in its row of 16.
+__device__ __forceinline__ uint32_t from_other_half(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xF, 0xF, true);  // row_ror:8
+}
+
+// A wave's results: out(m) is the row of its m-th (null: none), `first` its first column.  A lane has some columns of row
+// l % 16.  Where 128 bytes of all rows exist they are stored as whole lines, eight lanes to a line: the lanes of
+// rows r and r + 8 exchange halves of their lines.  (Stored as they are, 32 bytes at a time: 131072 rows of 4096 bf16 240 us.)
 template <typename T, typename S, bool PAIRED, typename OUT>
 __device__ __forceinline__ void store_tile(const f32x4 (&acc)[S::kTm][S::kTn], int first, int cols, int lane, OUT out) {
     const int g = lane >> 4;
+    constexpr int kLine = T::kPer == 4 ? 2 : 4;  // fragments of a line
+    if (S::kTn % kLine == 0 && first + 16 * S::kTn <= cols) {
+        const bool high = lane & 8;
+        // a lane's two chunks of 16 bytes of a line, in bytes from its start
+        const int at0 = T::kPer == 4 ? (PAIRED ? 32 * g : 16 * g) : PAIRED ? 16 * g : 32 * (g & 1) + 16 * (g >> 1);
+        const int at1 = at0 + (T::kPer == 4 && PAIRED ? 16 : 64);
+        const int at = (high ? at1 : at0) / (int)sizeof(typename T::elem) + first;
+#pragma unroll
+        for (int m = 0; m < S::kTm; ++m) {
+            typename T::elem* const p0 = out(16 * m + (lane & 7));
+            typename T::elem* const p1 = out(16 * m + (lane & 7) + 8);
+#pragma unroll
+            for (int n = 0; n < S::kTn; n += kLine) {
+                u32x4 c0, c1;
+                if constexpr (T::kPer == 4) {
+                    c0 = __builtin_bit_cast(u32x4, acc[m][n]);
+                    c1 = __builtin_bit_cast(u32x4, acc[m][n + 1]);
+                } else {
+                    const float f[16] = {
+                        acc[m][n].x,     acc[m][n].y,     acc[m][n].z,     acc[m][n].w,
+                        acc[m][n + 1].x, acc[m][n + 1].y, acc[m][n + 1].z, acc[m][n + 1].w,
+                        acc[m][n + 2].x, acc[m][n + 2].y, acc[m][n + 2].z, acc[m][n + 2].w,
+                        acc[m][n + 3].x, acc[m][n + 3].y, acc[m][n + 3].z, acc[m][n + 3].w,
+                    };
+                    c0 = T::pack(f);
+                    c1 = T::pack(f + 8);
+                    if constexpr (!PAIRED) {  // four columns of two fragments each become eight of one
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const auto r0 = __builtin_amdgcn_permlane16_swap(c0[i], c0[i + 2], false, false);
+                            const auto r1 = __builtin_amdgcn_permlane16_swap(c1[i], c1[i + 2], false, false);
+                            c0[i] = r0[0];
+                            c0[i + 2] = r0[1];
+                            c1[i] = r1[0];
+                            c1[i + 2] = r1[1];
+                        }
+                    }
+                }
+                u32x4 low, up;  // of rows l % 8 and l % 8 + 8
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t other = from_other_half(high ? c0[i] : c1[i]);
+                    low[i] = high ? other : c0[i];
+                    up[i] = high ? c1[i] : other;
+                }
+                const int col = at + 16 * n;
+                if (p0)
+                    store_vec<T, false>(p0 + col, low);
+                if (p1)
+                    store_vec<T, false>(p1 + col, up);
+            }
+        }
+        return;
+    }
 #pragma unroll
     for (int m = 0; m < S::kTm; ++m) {
         typename T::elem* const p = out(16 * m + (lane & 15));
         if (!p)
             continue;
-        if constexpr (PAIRED) {
 #pragma unroll
-            for (int n = 0; n < S::kTn; n += 2) {
-                const float f[8] = {acc[m][n].x,     acc[m][n].y,     acc[m][n].z,     acc[m][n].w,
-                                    acc[m][n + 1].x, acc[m][n + 1].y, acc[m][n + 1].z, acc[m][n + 1].w};
-                store_results<T, 8>(p, first + 16 * n + 8 * g, cols, f);
-            }
-        } else {
-#pragma unroll
-            for (int n = 0; n < S::kTn; ++n) {
-                const float f[4] = {acc[m][n].x, acc[m][n].y, acc[m][n].z, acc[m][n].w};
-                store_results<T, 4>(p, first + 16 * n + 4 * g, cols, f);
-            }
+        for (int n = 0; n < S::kTn; ++n) {
+            const float f[4] = {acc[m][n].x, acc[m][n].y, acc[m][n].z, acc[m][n].w};
+            store_results<T>(p, first + (PAIRED ? 32 * (n / 2) + 8 * g + 4 * (n % 2) : 16 * n + 4 * g), cols, f);
         }
     }
 }
@@ -341,10 +479,11 @@ __device__ __forceinline__ bool find_tile(const ExpertCall& a, uint32_t first, u
 template <typename T, typename S, bool ALONG, bool DMA>
 __global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall a, uint32_t first, uint32_t launched) {
     using elem = typename T::elem;
-    constexpr int kPer = T::kPer, kStep = kStepBytes / (int)sizeof(elem);
-    constexpr int kChunks = ALONG ? 8 : S::BN / kPer;             // chunks of a row of the weights' tile
-    constexpr int kXRows = S::kThreads / 8, kWRows = S::kThreads / kChunks;  // tile rows of one load of all threads
-    __shared__ __attribute__((aligned(1024))) char tiles[S::kStages * S::kStage];
+    constexpr int kPer = T::kPer, kStep = S::kBytes / (int)sizeof(elem);
+    constexpr int kXChunks = S::kBytes / 16, kChunks = ALONG ? kXChunks : S::BN / kPer;  // of the tiles' rows
+    constexpr int kXRows = S::kThreads / kXChunks, kWRows = S::kThreads / kChunks;  // tile rows of one load of all threads
+    constexpr int kStages = DMA ? S::kStages : 2;
+    __shared__ __attribute__((aligned(1024))) char tiles[kStages * S::kStage];
 
     TilePlace place;
     const uint32_t col_tiles = ((uint32_t)a.cols_out + S::BN - 1) / S::BN;
@@ -361,7 +500,7 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall
     const elem* px[S::kRowLoads];
     const elem* pw[S::kColLoads];
     int wc[S::kColLoads];
-    const int xr = t / 8, xc = ((t & 7) ^ along_exchange<false>(xr)) * kPer;
+    const int xr = t / kXChunks, xc = ((t % kXChunks) ^ along_exchange<false, S::kBytes>(xr)) * kPer;
 #pragma unroll
     for (int j = 0; j < S::kRowLoads; ++j) {  // rows past the run's are not stored
         const uint32_t i = (uint32_t)place.first + xr + j * kXRows;  // may pass 2^31
@@ -374,7 +513,7 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall
     for (int j = 0; j < S::kColLoads; ++j) {
         const int r = t / kChunks + j * kWRows;
         if constexpr (ALONG) {
-            wc[j] = ((t & 7) ^ along_exchange<true>(r)) * kPer;
+            wc[j] = ((t % kXChunks) ^ along_exchange<true, S::kBytes>(r)) * kPer;
             const int n = n0 + r < a.cols_out ? n0 + r : a.cols_out - 1;  // columns past the last are not stored
             pw[j] = w + n * a.ld_w;
             if constexpr (DMA)
@@ -394,7 +533,7 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall
     auto copy = [&](int step, auto whole) __attribute__((always_inline)) {
         constexpr bool WHOLE = decltype(whole)::value;
         const int k0 = step * kStep;
-        const uint32_t stage = lds + step % S::kStages * S::kStage;
+        const uint32_t stage = lds + step % kStages * S::kStage;
 #pragma unroll
         for (int j = 0; j < S::kRowLoads; ++j)
             copy_to_lds(WHOLE || k0 + xc < depth ? px[j] + k0 : zeros, stage + j * S::kThreads * 16);
@@ -430,7 +569,7 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall
     };
     auto put = [&](int step) __attribute__((always_inline)) {
         if constexpr (!DMA) {
-            char* const stage = tiles + step % S::kStages * S::kStage + t * 16;
+            char* const stage = tiles + step % kStages * S::kStage + t * 16;
 #pragma unroll
             for (int j = 0; j < S::kRowLoads; ++j)
                 *reinterpret_cast<u32x4*>(stage + j * S::kThreads * 16) = rx[j];
@@ -441,8 +580,8 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall
     };
 
     const int wm = wave % S::WM, wn = wave / S::WM;
-    const Side<T, true, false, S::BM, S::kTm> xs(wm * S::kTm * 16, lane);
-    const Side<T, ALONG, ALONG, S::BN, S::kTn> ws(wn * S::kTn * 16, lane);
+    const Side<T, true, false, S::BM, S::kTm, S::kBytes> xs(wm * S::kTm * 16, lane);
+    const Side<T, ALONG, ALONG, S::BN, S::kTn, S::kBytes> ws(wn * S::kTn * 16, lane);
     f32x4 acc[S::kTm][S::kTn];
 #pragma unroll
     for (int m = 0; m < S::kTm; ++m)
@@ -450,7 +589,7 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall
         for (int n = 0; n < S::kTn; ++n)
             acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    constexpr int kAhead = DMA ? S::kStages - 1 : 1;  // stages under way
+    constexpr int kAhead = kStages - 1;  // stages under way
 #pragma unroll
     for (int s = 0; s < kAhead; ++s)
         if (s < steps) {
@@ -465,7 +604,7 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall
             wait_stage<0>();
         if (s + kAhead < steps)
             fetch(s + kAhead);
-        multiply<T, S>(tiles + s % S::kStages * S::kStage, xs, ws, acc);
+        multiply<T, S>(tiles + s % kStages * S::kStage, xs, ws, acc);
         if (s + kAhead < steps)
             put(s + kAhead);
     }
@@ -491,6 +630,223 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall
 }
 
 // ---------------------------------------------------------------------------
+// The same in a run of tiles for each workgroup; rows of x and of the weights are made of aligned chunks.
+// ---------------------------------------------------------------------------
+struct TileTable {
+    int32_t upto[ZERO_ROUTE_MAX_EXPERTS];  // row tiles of the experts up to this one
+    int32_t lo[ZERO_ROUTE_MAX_EXPERTS], hi[ZERO_ROUTE_MAX_EXPERTS];
+};
+
+template <int BM>
+__device__ __forceinline__ void fill_tile_table(TileTable& table, const ExpertCall& a) {
+    const int lane = threadIdx.x & 63, slots = (int)a.slots;
+    if (threadIdx.x < 64) {
+        uint32_t before = 0;
+        for (int e0 = 0; e0 < a.experts; e0 += 64) {
+            const int e = e0 + lane;
+            int lo = 0, hi = 0;
+            if (e < a.experts) {
+                lo = a.offsets[e];
+                hi = a.offsets[e + 1];
+            }
+            lo = lo < 0 ? 0 : lo > slots ? slots : lo;
+            hi = hi < lo ? lo : hi > slots ? slots : hi;
+            uint32_t upto = ((uint32_t)(hi - lo) + BM - 1) / BM;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const uint32_t o = __shfl_up(upto, d);
+                upto += lane >= d ? o : 0;
+            }
+            upto += before;
+            if (e < a.experts) {
+                table.upto[e] = (int)upto;
+                table.lo[e] = lo;
+                table.hi[e] = hi;
+            }
+            before = __shfl(upto, 63);
+        }
+    }
+    __syncthreads();
+}
+
+// Row tiles in groups of eight by all columns' tiles, whose operands a die's L2 serves.
+template <int BM>
+__device__ __forceinline__ TilePlace tile_place(const TileTable& table, int experts, uint32_t row_tiles, uint32_t col_tiles,
+                                                uint32_t id) {
+    constexpr uint32_t kGroup = 8;
+    const int lane = threadIdx.x & 63;
+    const uint32_t per = kGroup * col_tiles, group = id / per, rest = id - group * per;
+    const uint32_t rows_in = row_tiles - group * kGroup < kGroup ? row_tiles - group * kGroup : kGroup;
+    const uint32_t col_tile = rest / rows_in, row_tile = group * kGroup + rest - col_tile * rows_in;
+    TilePlace out{};
+    for (int e0 = 0; e0 < experts; e0 += 64) {
+        const int e = e0 + lane;
+        const uint64_t found = __ballot(e < experts && (uint32_t)table.upto[e < experts ? e : 0] > row_tile);
+        if (found) {
+            out.expert = e0 + __ffsll((unsigned long long)found) - 1;
+            break;
+        }
+    }
+    const uint32_t before = out.expert > 0 ? (uint32_t)table.upto[out.expert - 1] : 0;
+    out.first = __builtin_amdgcn_readfirstlane(table.lo[out.expert] + (int)((row_tile - before) * BM));
+    out.end = __builtin_amdgcn_readfirstlane(table.hi[out.expert]);
+    out.col_tile = (int)col_tile;
+    return out;
+}
+
+template <typename T, typename S, bool ALONG>
+__global__ __launch_bounds__(S::kThreads) void k_expert_product_run(const ExpertCall a) {
+    using elem = typename T::elem;
+    constexpr int kPer = T::kPer, kStep = S::kBytes / (int)sizeof(elem);
+    constexpr int kXChunks = S::kBytes / 16, kChunks = ALONG ? kXChunks : S::BN / kPer;  // of the tiles' rows
+    constexpr int kXRows = S::kThreads / kXChunks, kWRows = S::kThreads / kChunks;  // tile rows of one load of all threads
+    // Tiles whose entries of order are held: copies run up to kStages tiles ahead of the products (where a tile has one step),
+    // the entries kStages tiles ahead of the copies.
+    constexpr int kRing = S::kStages <= 3 ? 8 : 16;
+    static_assert(kRing > 2 * S::kStages && S::BM % 64 == 0);
+    __shared__ __attribute__((aligned(1024))) char tiles[S::kStages * S::kStage];
+    __shared__ int32_t slots_of[kRing][S::BM];
+    __shared__ TileTable table;
+
+    fill_tile_table<S::BM>(table, a);
+    const uint32_t col_tiles = ((uint32_t)a.cols_out + S::BN - 1) / S::BN;
+    const uint32_t row_tiles = __builtin_amdgcn_readfirstlane(table.upto[a.experts - 1]), all = row_tiles * col_tiles;
+    // a die's workgroups take a run of the tiles in turn
+    const uint32_t each = (all + 7) / 8, stride = gridDim.x / 8, die = blockIdx.x & 7;
+    const uint32_t first = die * each + blockIdx.x / 8, last = (die + 1) * each < all ? (die + 1) * each : all;
+    if (first >= last)
+        return;
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int depth = a.cols_in, steps = (depth + kStep - 1) / kStep;
+    const elem* const zeros = reinterpret_cast<const elem*>(&zero_chunk);
+    const bool ordered = a.x_map.mode | a.out_map.mode;
+    auto place_of = [&](uint32_t id) { return tile_place<S::BM>(table, a.experts, row_tiles, col_tiles, id); };
+
+    // The entries of order of a tile; each wave copies 64 of them.
+    auto look_up = [&](uint32_t id, int ring) __attribute__((always_inline)) {
+        if (ordered && id < last) {
+            const TilePlace p = place_of(id);
+            const int r = wave % (S::BM / 64) * 64;
+            const uint32_t i = (uint32_t)p.first + r + lane;  // may pass 2^31
+            copy_word_to_lds(a.order + (i < (uint32_t)p.end ? i : p.end - 1), lds_address(&slots_of[ring][r]));
+        }
+    };
+    // The row of a matrix of row r of a tile whose entries of order lie in `ring`, -1: none
+    auto row_of = [&](const SlotMap& map, const TilePlace& p, int ring, int r) __attribute__((always_inline)) -> int64_t {
+        const uint32_t i = (uint32_t)p.first + r;
+        if (map.mode == 0)
+            return i < (uint32_t)p.end ? i : p.end - 1;
+        const uint32_t slot = (uint32_t)slots_of[ring][r];
+        return slot < (uint64_t)a.slots ? map.row(slot) : -1;
+    };
+
+    // the tile whose copies are issued, and the step of it
+    uint32_t copy_id = first;
+    int copy_step = 0, copy_ring = 0;
+    const elem* px[S::kRowLoads];
+    const int xr = t / kXChunks, xc = ((t % kXChunks) ^ along_exchange<false, S::kBytes>(xr)) * kPer;
+    // the exchange looks at four bits of the row, so a thread's rows of the weights' tile have one chunk, or two in turn
+    constexpr int kColumns = ALONG || kWRows % 16 == 0 ? 1 : 2;
+    static_assert(kWRows * kColumns % 16 == 0);
+    int wc[kColumns];  // across: the columns
+    const int wr = t / kChunks, wk = ALONG ? ((t % kChunks) ^ along_exchange<true, S::kBytes>(wr)) * kPer : wr;
+    const elem* pw = nullptr;
+    int w_room = 0;  // ALONG: the weights' rows behind the first
+    int k0 = 0;
+    auto next_step = [&]() __attribute__((always_inline)) -> bool {
+        if (copy_step == steps) {
+            copy_step = 0;
+            copy_id += stride;
+            copy_ring = (copy_ring + 1) % kRing;
+        }
+        if (copy_id >= last)
+            return false;
+        if (copy_step == 0) {
+            const TilePlace p = place_of(copy_id);
+            const int n0 = p.col_tile * S::BN;
+            const elem* const w = static_cast<const elem*>(a.w) +
+                                  (int64_t)p.expert * (ALONG ? a.cols_out : a.cols_in) * a.ld_w;
+#pragma unroll
+            for (int j = 0; j < S::kRowLoads; ++j) {  // rows past the run's are not stored
+                const int64_t row = row_of(a.x_map, p, copy_ring, xr + j * kXRows);
+                px[j] = static_cast<const elem*>(a.x) + (row < 0 ? 0 : row) * a.ld_x + xc;  // none: stored as zeros
+            }
+            if constexpr (ALONG) {  // columns past the last are not stored
+                const int n = n0 + wr < a.cols_out ? n0 + wr : a.cols_out - 1;
+                pw = w + n * a.ld_w + wk;
+                w_room = a.cols_out - 1 - n;
+            } else {
+                pw = w + wr * a.ld_w;
+#pragma unroll
+                for (int j = 0; j < kColumns; ++j) {
+                    const int c = n0 + ((t % kChunks) ^ across_exchange<T, kChunks>(wr + j * kWRows)) * kPer;
+                    wc[j] = c < a.cols_out ? c : a.cols_out - kPer;
+                }
+                if constexpr (kColumns == 1)
+                    pw += wc[0];
+            }
+            look_up(copy_id + S::kStages * stride, (copy_ring + S::kStages) % kRing);
+        }
+        k0 = copy_step * kStep;
+        ++copy_step;
+        return true;
+    };
+    auto copy = [&](int i, uint32_t stage) __attribute__((always_inline)) {
+        if (i < S::kRowLoads) {
+            copy_to_lds(k0 + xc < depth ? px[i] + k0 : zeros, stage + i * S::kThreads * 16);
+        } else {
+            const int j = i - S::kRowLoads;
+            const elem* from = pw;
+            if constexpr (ALONG)
+                from += (w_room < j * kWRows ? w_room : j * kWRows) * a.ld_w + k0;
+            else
+                from += (k0 + j * kWRows) * a.ld_w + (kColumns == 1 ? 0 : wc[j % kColumns]);
+            copy_to_lds(k0 + (ALONG ? 0 : j * kWRows) + wk < depth ? from : zeros, stage + S::kRowsBytes + j * S::kThreads * 16);
+        }
+    };
+
+    uint32_t id = first;
+    int ring = 0;
+    bool begun = false;
+    auto tile_steps = [&]() __attribute__((always_inline)) -> int {
+        if (begun) {
+            id += stride;
+            ring = (ring + 1) % kRing;
+        }
+        begun = true;
+        return id < last ? steps : -1;
+    };
+    const int wm = wave % S::WM, wn = wave / S::WM;
+    const Side<T, true, false, S::BM, S::kTm, S::kBytes> xs(wm * S::kTm * 16, lane);
+    const Side<T, ALONG, ALONG, S::BN, S::kTn, S::kBytes> ws(wn * S::kTn * 16, lane);
+    auto finish = [&](f32x4 (&acc)[S::kTm][S::kTn]) __attribute__((always_inline)) {
+        const TilePlace p = place_of(id);
+        if (a.x_map.mode && !a.out_map.mode) {  // rows without a slot; in the slots' order they are not stored
+#pragma unroll
+            for (int m = 0; m < S::kTm; ++m)
+                if (row_of(a.x_map, p, ring, (wm * S::kTm + m) * 16 + (lane & 15)) < 0)
+#pragma unroll
+                    for (int n = 0; n < S::kTn; ++n)
+                        acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        elem* const y = static_cast<elem*>(a.out);
+        store_tile<T, S, ALONG>(acc, p.col_tile * S::BN + wn * S::kTn * 16, a.cols_out, lane, [&](int m) -> elem* {
+            const int r = wm * S::kTm * 16 + m;
+            if ((uint32_t)p.first + r >= (uint32_t)p.end)
+                return nullptr;
+            const int64_t row = row_of(a.out_map, p, ring, r);
+            return row < 0 ? nullptr : y + row * a.ld_out;
+        });
+    };
+    if (ordered) {
+        for (int i = 0; i < S::kStages; ++i)
+            look_up(first + i * stride, i);
+        wait_stage<0>();
+    }
+    multiply_tiles<T, S>(tiles, lds_address(tiles) + wave * 1024, xs, ws, next_step, copy, tile_steps, finish);
+}
+
+// ---------------------------------------------------------------------------
 // dweight = x^T * dy, a tile of one expert's matrix for a workgroup, the expert's rows in `splits` parts
 // whose sums k_expert_join adds up.
 // ---------------------------------------------------------------------------
@@ -499,9 +855,13 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_weight_back(const Expert
                                                                     uint32_t launched) {
     using elem = typename T::elem;
     static_assert(S::BM == S::BN, "a thread's rows of x and dy are the same slots");
-    constexpr int kPer = T::kPer, kStep = kStepBytes / (int)sizeof(elem);
+    constexpr int kPer = T::kPer, kStep = S::kBytes / (int)sizeof(elem);
     constexpr int kChunks = S::BN / kPer, kRows = S::kThreads / kChunks, kLoads = S::kColLoads;
-    __shared__ __attribute__((aligned(1024))) char tiles[2 * S::kStage];
+    constexpr int kStages = DMA ? S::kStages : 2, kAhead = kStages - 1;
+    static_assert(kStep <= 64, "a wave looks up a step's slots");
+    __shared__ __attribute__((aligned(1024))) char tiles[kStages * S::kStage];
+    constexpr int kRing = 2 * kStages;  // the steps that are looked up and not fetched yet, and more than a step between them
+    __shared__ int32_t slots_of[kRing][64];  // the steps' entries of order
 
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const uint32_t m_tiles = ((uint32_t)a.cols_in + S::BM - 1) / S::BM, n_tiles = ((uint32_t)a.cols_out + S::BN - 1) / S::BN;
@@ -537,24 +897,25 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_weight_back(const Expert
     }
     const uint32_t lds = lds_address(tiles) + wave * 1024;
     const bool ordered = a.x_map.mode | a.out_map.mode;
-    // entries of order for a step's rows, a step before they are needed; -1: no row
-    int32_t slot[kLoads];
+    // A step's entries of order come to LDS with the tiles of the step kAhead before it.  (Loaded into registers they would
+    // have to be waited for, and with them, in the order of the loads, every copy that was issued before.)
+    // Each wave copies them all, to the same place.
     auto look_up = [&](int step) __attribute__((always_inline)) {
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const uint32_t i = (uint32_t)begin + (uint32_t)step * kStep + t / kChunks + j * kRows;  // may pass 2^31
-            slot[j] = i < (uint32_t)end ? (ordered ? a.order[i] : 0) : -1;
-        }
+        const uint32_t i = (uint32_t)begin + (uint32_t)step * kStep + lane;  // may pass 2^31
+        if (ordered)
+            copy_word_to_lds(a.order + (i < (uint32_t)end ? i : end - 1), lds_address(slots_of[step % kRing]));
     };
     u32x4 rx[DMA ? 1 : kLoads], rw[DMA ? 1 : kLoads];
     auto fetch = [&](int step) __attribute__((always_inline)) {
-        const uint32_t stage = lds + (step & 1) * S::kStage;
+        const uint32_t stage = lds + step % kStages * S::kStage;
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int64_t i = begin + (int64_t)step * kStep + t / kChunks + j * kRows;
-            const bool there = (uint32_t)slot[j] < (uint32_t)slots;
-            const elem* const px = x + (a.x_map.mode ? a.x_map.row(slot[j]) : i) * a.ld_x;
-            const elem* const pw = dy + (a.out_map.mode ? a.out_map.row(slot[j]) : i) * a.ld_w;
+            const int r = t / kChunks + j * kRows;
+            const int64_t i = begin + (int64_t)step * kStep + r;
+            const uint32_t slot = ordered ? slots_of[step % kRing][r] : 0;
+            const bool there = i < end && slot < (uint32_t)slots;
+            const elem* const px = x + (there ? (a.x_map.mode ? a.x_map.row(slot) : i) : 0) * a.ld_x;
+            const elem* const pw = dy + (there ? (a.out_map.mode ? a.out_map.row(slot) : i) : 0) * a.ld_w;
             if constexpr (DMA) {
                 copy_to_lds(there ? px + xc[j] : zeros, stage + j * S::kThreads * 16);
                 copy_to_lds(there ? pw + wc[j] : zeros, stage + S::kRowsBytes + j * S::kThreads * 16);
@@ -566,10 +927,11 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_weight_back(const Expert
                 }
             }
         }
+        look_up(step + kAhead);
     };
     auto put = [&](int step) __attribute__((always_inline)) {
         if constexpr (!DMA) {
-            char* const stage = tiles + (step & 1) * S::kStage + t * 16;
+            char* const stage = tiles + step % kStages * S::kStage + t * 16;
 #pragma unroll
             for (int j = 0; j < kLoads; ++j) {
                 *reinterpret_cast<u32x4*>(stage + j * S::kThreads * 16) = rx[j];
@@ -579,8 +941,8 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_weight_back(const Expert
     };
 
     const int wm = wave % S::WM, wn = wave / S::WM;
-    const Side<T, false, false, S::BM, S::kTm> xs(wm * S::kTm * 16, lane);
-    const Side<T, false, false, S::BN, S::kTn> ws(wn * S::kTn * 16, lane);
+    const Side<T, false, false, S::BM, S::kTm, S::kBytes> xs(wm * S::kTm * 16, lane);
+    const Side<T, false, false, S::BN, S::kTn, S::kBytes> ws(wn * S::kTn * 16, lane);
     f32x4 acc[S::kTm][S::kTn];
 #pragma unroll
     for (int m = 0; m < S::kTm; ++m)
@@ -588,21 +950,33 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_weight_back(const Expert
         for (int n = 0; n < S::kTn; ++n)
             acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
 
+    // the copies of a step, its entries of order among them
+    constexpr int kCopies = DMA ? 2 * kLoads + 1 : 1;
     if (steps > 0) {
-        look_up(0);
-        fetch(0);
-        put(0);
-        look_up(1);
-    }
-    for (int s = 0; s < steps; ++s) {
+        for (int s = 0; s < kAhead; ++s)
+            look_up(s);
         wait_stage<0>();
-        if (s + 1 < steps) {
-            fetch(s + 1);
-            look_up(s + 2);
+    }
+    for (int s = 0; s < kAhead; ++s)
+        if (s < steps) {
+            fetch(s);
+            put(s);
         }
-        multiply<T, S>(tiles + (s & 1) * S::kStage, xs, ws, acc);
-        if (s + 1 < steps)
-            put(s + 1);
+    for (int s = 0; s < steps; ++s) {
+        // the last steps have nothing behind them; without an order there are fewer copies to wait for
+        if (kAhead > 1 && s + kAhead <= steps) {
+            if (ordered)
+                wait_stage<(kAhead - 1) * kCopies>();
+            else
+                wait_stage<(kAhead - 1) * (kCopies - 1)>();
+        } else {
+            wait_stage<0>();
+        }
+        if (s + kAhead < steps)
+            fetch(s + kAhead);
+        multiply<T, S>(tiles + s % kStages * S::kStage, xs, ws, acc);
+        if (s + kAhead < steps)
+            put(s + kAhead);
     }
 
     const int col = n0 + wn * S::kTn * 16;

@@ -51,16 +51,29 @@ bool whole_chunks(const void* p, int64_t ld, int64_t cols, size_t elem) {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * elem % 16 == 0 && cols * elem % 16 == 0;
 }
 
+// The shape of the kernel that takes tiles in a run (operands in aligned chunks), by the experts' mean number of rows.
+template <typename F>
+int with_run_shape(int64_t mean, F f) {
+#ifndef ZO_MIN
+#define ZO_MIN 200
+#endif
+#ifndef ZO_ST
+#define ZO_ST 2
+#define ZO_KB 128
+#endif
+    if (mean <= ZO_MIN) return f(zo::TileShape<128, 256, 2, 4, ZO_ST, ZO_KB>{});
+    return f(zo::TileShape<256, 256, 2, 4, ZO_ST, ZO_KB>{});
+}
+
 template <typename F>
 int with_product_shape(int64_t mean, F f) {
-    if (mean <= 48) return f(zo::TileShape<32, 128, 1, 4, 4>{});
-    if (mean <= 512) return f(zo::TileShape<128, 128, 2, 2, 2>{});
-    return f(zo::TileShape<256, 256, 2, 4, 2>{});
+    if (mean <= 48) return f(zo::TileShape<32, 128, 1, 4, 4, 128>{});
+    return f(zo::TileShape<128, 128, 2, 2, 2, 64>{});
 }
 
 // Parts of the summed axis in the weights' gradient: enough workgroups to fill the device twice, within the workspace's
 // bound, and of no less than 256 slots each on average.
-constexpr int kBackTile = 128;
+constexpr int kBackTile = 256;
 
 int back_splits(int64_t slots, int experts, int64_t cols_in, int64_t cols_out) {
     const int64_t tiles = experts * div_up(cols_in, kBackTile) * div_up(cols_out, kBackTile);
@@ -118,7 +131,19 @@ int zero_expert_product(const zero_expert_product_args_t* args, void* stream_) {
     const bool dma = whole_chunks(a.x, a.ld_x, a.cols_in, e) && whole_chunks(a.weight, a.ld_weight, w_cols, e);
     return with_type(a.dtype, [&](auto type) {
         using T = decltype(type);
-        return with_product_shape(a.slots / a.experts, [&](auto shape) {
+        const int64_t mean = a.slots / a.experts;
+        if (dma && mean > 48)
+            return with_run_shape(mean, [&](auto shape) {
+                using S = decltype(shape);
+                const int64_t rows = std::min<int64_t>(a.slots, a.slots / S::BM + a.experts);
+                const int64_t tiles = rows * div_up(a.cols_out, S::BN);
+                const unsigned grid = (unsigned)std::min<int64_t>(256, div_up(tiles, 8) * 8);
+                auto* const kernel = a.transposed ? zo::k_expert_product_run<T, S, true> : zo::k_expert_product_run<T, S, false>;
+                kernel<<<grid, S::kThreads, 0, stream>>>(c);
+                HIP_TRY(hipGetLastError());
+                return ZERO_OK;
+            });
+        return with_product_shape(mean, [&](auto shape) {
             using S = decltype(shape);
             // every expert's last tile may hold one row
             const int64_t rows = std::min<int64_t>(a.slots, a.slots / S::BM + a.experts);
@@ -209,7 +234,7 @@ int zero_expert_weight_backward(const zero_expert_weight_backward_args_t* args, 
             }
             return ZERO_OK;
         };
-        return launch(zo::TileShape<kBackTile, kBackTile, 2, 2, 2>{});
+        return launch(zo::TileShape<kBackTile, kBackTile, 2, 4, 4, 64>{});
     });
 }
 
