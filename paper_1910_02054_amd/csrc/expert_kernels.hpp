@@ -58,11 +58,11 @@ struct ExpertCall {
     int64_t ld_w;
     void* out;             // y, or dweight
     int64_t ld_out;
-    float* partial;        // [splits, experts, cols_in, cols_out]
+    float* partial;        // [parts, cols_in, cols_out]
     int64_t slots;
     int32_t experts;
     int32_t cols_in, cols_out;
-    int32_t splits;
+    int32_t part;          // rows of a part of the weights' gradient's sums; 0: an expert's rows are one part
     SlotMap x_map, out_map;  // of x, and of y or dy
 };
 
@@ -223,13 +223,17 @@ __device__ __forceinline__ void wait_stage() {
 //   finish(acc)          stores a tile's results
 // A step is two halves of kTm groups of products, one of the rows' fragments with all of the columns'.  Fragments are read
 // kLead groups before they are needed, so kLead groups before a step's end its stage is free for the copies of step s + kStages:
-// there all waves meet, and step s + 1 has landed.
-template <typename T, typename S, typename XS, typename WS, typename NEXT, typename COPY, typename STEPS, typename FINISH>
+// there all waves meet, and step s + 1 has landed.  EARLY: copies of a stage that is free sooner, those of the columns'
+// first half where its rows are places of the axis; they begin kLead groups before the half's end, and the columns' second half
+// need not have landed before.  Copies 0 to EARLY - 1 are these, the last EARLY those of the second half.
+template <typename T, typename S, int EARLY, typename XS, typename WS, typename NEXT, typename COPY, typename STEPS,
+          typename FINISH>
 __device__ __forceinline__ void multiply_tiles(const char* tiles, uint32_t lds, const XS& xs, const WS& ws, NEXT next_step,
                                                COPY copy, STEPS tile_steps, FINISH finish) {
-    constexpr int kLead = S::kTm / 2, kHalves = S::kBytes / 64, kGroups = kHalves * S::kTm;
-    static_assert(S::kTm % 2 == 0 && S::kTn % kLead == 0, "whole fragments a group");
-    constexpr int kReads = S::kTn / kLead, kCopyRate = (S::kCopies + kLead - 1) / kLead;
+    constexpr int kLead = S::kTm / 2, kGroups = 2 * S::kTm;
+    static_assert(S::kBytes == 128 && S::kTm % 2 == 0 && S::kTn % kLead == 0, "two halves, whole fragments a group");
+    constexpr int kReads = S::kTn / kLead, kCopyRate = (S::kCopies - EARLY + kLead - 1) / kLead;
+    constexpr int kEarlyRate = (EARLY + kLead - 1) / kLead;
     bool more = false;
 #pragma unroll
     for (int s = 0; s < S::kStages; ++s) {
@@ -240,7 +244,7 @@ __device__ __forceinline__ void multiply_tiles(const char* tiles, uint32_t lds, 
                 copy(i, lds + s * S::kStage);
     }
     if (more)
-        wait_stage<(S::kStages - 1) * S::kCopies>();
+        wait_stage<(S::kStages - 1) * S::kCopies + EARLY>();
     else
         wait_stage<0>();
     u32x4 xf[S::kTm], wf[S::kTn], wn[S::kTn];
@@ -264,26 +268,43 @@ __device__ __forceinline__ void multiply_tiles(const char* tiles, uint32_t lds, 
 #pragma unroll
             for (int q = 0; q < kGroups; ++q) {
                 const int m = q % S::kTm, ahead = (q + kLead) % kGroups;
-                if (q == kGroups - kLead) {
-                    // in the order of the loads: later ones that are under way can only make the wait longer
+                // waits in the order of the loads: later ones that are under way can only make them longer
+                if (EARLY > 0 && q == S::kTm - kLead) {
                     if (more)
-                        wait_stage<(S::kStages - 2) * S::kCopies>();
+                        wait_stage<(S::kStages - 1) * S::kCopies>();
+                    else
+                        wait_stage<0>();
+                    more = more && next_step();
+                }
+                if (q == kGroups - kLead) {
+                    if (more)
+                        wait_stage<(S::kStages - 2) * S::kCopies + 2 * EARLY>();
                     else
                         wait_stage<0>();
                     at = at + 1 == S::kStages ? 0 : at + 1;
                     from = tiles + at * S::kStage;
-                    more = more && next_step();
+                    if (EARLY == 0)
+                        more = more && next_step();
                 }
                 xf[ahead % S::kTm] = xs.load(from, ahead % S::kTm, ahead / S::kTm);
-                if (m >= kLead)
+                if (m >= kLead) {
 #pragma unroll
                     for (int i = 0; i < kReads; ++i)
                         wn[(m - kLead) * kReads + i] =
                             ws.load(from + S::kRowsBytes, (m - kLead) * kReads + i, ahead / S::kTm);
-                if (q >= kGroups - kLead && more)
+                    if (more) {
+                        if (q < S::kTm) {
 #pragma unroll
-                    for (int i = (m - kLead) * kCopyRate; i < (m - kLead + 1) * kCopyRate && i < S::kCopies; ++i)
-                        copy(i, stage);
+                            for (int i = (m - kLead) * kEarlyRate; i < (m - kLead + 1) * kEarlyRate && i < EARLY; ++i)
+                                copy(i, stage);
+                        } else {
+#pragma unroll
+                            for (int i = EARLY + (m - kLead) * kCopyRate;
+                                 i < EARLY + (m - kLead + 1) * kCopyRate && i < S::kCopies; ++i)
+                                copy(i, stage);
+                        }
+                    }
+                }
 #pragma unroll
                 for (int n = 0; n < S::kTn; ++n)
                     acc[m][n] = mma<T>(wf[n], xf[m], acc[m][n]);
@@ -396,8 +417,8 @@ __device__ __forceinline__ void store_tile(const f32x4 (&acc)[S::kTm][S::kTn], i
 }
 
 // ---------------------------------------------------------------------------
-// Which tile a workgroup takes.  The host knows no expert's number of rows, so it launches as many as there
-// can be; each workgroup adds up the experts' tiles, and those past the last have nothing to do.
+// Which tiles a workgroup takes.  The host knows no expert's number of rows, so every workgroup adds up the experts' tiles
+// first; where there are more workgroups than tiles, those past the last have nothing to do.
 // Workgroups go to the eight dies in turn, so that numbering gives each die a run of the tiles: eight
 // rows' tiles by all columns' tiles, whose operands its L2 then serves.
 // ---------------------------------------------------------------------------
@@ -407,6 +428,78 @@ struct TilePlace {
     int col_tile;
 };
 
+struct TileTable {
+    uint32_t upto[ZERO_ROUTE_MAX_EXPERTS];  // row tiles, or parts, of the experts up to this one
+    int32_t begin[ZERO_ROUTE_MAX_EXPERTS + 1];  // their first rows; never falling
+};
+
+// tiles(rows), and cost(rows) into `costs` (may be null), are added up.
+template <typename TILES, typename COST>
+__device__ __forceinline__ void fill_tile_table(TileTable& table, uint32_t* costs, const ExpertCall& a, TILES tiles, COST cost) {
+    const int lane = threadIdx.x & 63, slots = (int)a.slots;
+    auto row = [&](int e) {
+        const int o = a.offsets[e];
+        return o < 0 ? 0 : o > slots ? slots : o;
+    };
+    if (threadIdx.x < 64) {
+        int begin = row(0);
+        uint32_t before = 0, spent = 0;
+        if (lane == 0)
+            table.begin[0] = begin;
+        for (int e0 = 0; e0 < a.experts; e0 += 64) {
+            const int e = e0 + lane;
+            int end = e < a.experts ? row(e + 1) : 0;
+            end = end < begin ? begin : end;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const int o = __shfl_up(end, d);
+                end = lane >= d && o > end ? o : end;
+            }
+            const int previous = __shfl_up(end, 1), rows = end - (lane ? previous : begin);
+            uint32_t n = e < a.experts ? tiles(rows) : 0, c = e < a.experts && costs ? cost(rows) : 0;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const uint32_t o = __shfl_up(n, d), q = __shfl_up(c, d);
+                n += lane >= d ? o : 0;
+                c += lane >= d ? q : 0;
+            }
+            if (e < a.experts) {
+                table.begin[e + 1] = end;
+                table.upto[e] = before + n;
+                if (costs)
+                    costs[e] = spent + c;
+            }
+            begin = __shfl(end, 63);
+            before += __shfl(n, 63);
+            spent += __shfl(c, 63);
+        }
+    }
+    __syncthreads();
+}
+
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
+
+// Tile `id` of rows by cols: row tiles in groups of eight by all columns' tiles, whose operands a die's L2 serves.
+__device__ __forceinline__ void grouped_tile(uint32_t id, uint32_t rows, uint32_t cols, uint32_t& row, uint32_t& col) {
+    constexpr uint32_t kGroup = 8;
+    const uint32_t per = kGroup * cols, group = id / per, rest = id - group * per;
+    const uint32_t rows_in = rows - group * kGroup < kGroup ? rows - group * kGroup : kGroup;
+    col = rest / rows_in;
+    row = group * kGroup + rest - col * rows_in;
+}
+
+// The first expert whose entry of a rising table is above `value`.
+__device__ __forceinline__ int expert_above(const uint32_t* upto, int experts, uint32_t value) {
+    const int lane = threadIdx.x & 63;
+    for (int e0 = 0; e0 < experts; e0 += 64) {
+        const int e = e0 + lane;
+        const uint64_t found = __ballot(e < experts && upto[e < experts ? e : 0] > value);
+        if (found)
+            return e0 + __ffsll((unsigned long long)found) - 1;
+    }
+    return experts - 1;
+}
+
 __device__ __forceinline__ uint32_t die_order(uint32_t id, uint32_t count) {
     const uint32_t each = (count + 7) / 8;
     const uint32_t t = (id & 7) * each + (id >> 3);
@@ -414,62 +507,17 @@ __device__ __forceinline__ uint32_t die_order(uint32_t id, uint32_t count) {
 }
 
 template <int BM>
-__device__ __forceinline__ bool find_tile(const ExpertCall& a, uint32_t first, uint32_t launched, uint32_t col_tiles,
-                                          TilePlace& out) {
-    const int lane = threadIdx.x & 63;
-    const int slots = (int)a.slots;
-    auto tiles_of = [&](int e, int& lo, int& hi) -> uint32_t {
-        lo = hi = 0;
-        if (e < a.experts) {
-            lo = a.offsets[e];
-            hi = a.offsets[e + 1];
-        }
-        lo = lo < 0 ? 0 : lo > slots ? slots : lo;
-        hi = hi < lo ? lo : hi > slots ? slots : hi;
-        return ((uint32_t)(hi - lo) + BM - 1) / BM;
-    };
-    int lo, hi;
-    uint32_t total = 0;
-    for (int e = lane; e < (a.experts + 63) / 64 * 64; e += 64)
-        total += tiles_of(e, lo, hi);
-    total = seg_reduce<64>(total, [](uint32_t p, uint32_t q) { return p + q; });
-    total = __builtin_amdgcn_readfirstlane(total);
-    const uint32_t all = total * col_tiles;
-    if (first >= all)
-        return false;
-    const uint32_t here = all - first < launched ? all - first : launched;
-    const uint32_t in_run = die_order(blockIdx.x, here);
-    if (in_run >= here)
-        return false;
-    const uint32_t id = first + in_run;
-    constexpr uint32_t kGroup = 8;
-    const uint32_t per = kGroup * col_tiles, group = id / per, rest = id - group * per;
-    const uint32_t rows_in = total - group * kGroup < kGroup ? total - group * kGroup : kGroup;
-    const uint32_t col_tile = rest / rows_in, row_tile = group * kGroup + rest - col_tile * rows_in;
-    uint32_t before = 0;
-    for (int e0 = 0; e0 < a.experts; e0 += 64) {
-        const uint32_t t = tiles_of(e0 + lane, lo, hi);
-        uint32_t upto = t;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const uint32_t o = __shfl_up(upto, d);
-            upto += lane >= d ? o : 0;
-        }
-        const uint32_t mine = row_tile - (before + upto - t);  // this workgroup's place among the expert's tiles
-        const uint64_t found = __ballot(mine < t);
-        if (found) {
-            const int l = __ffsll((unsigned long long)found) - 1;
-            out.expert = e0 + l;
-            out.first = __shfl(lo, l) + __shfl((int)mine, l) * BM;
-            out.end = __shfl(hi, l);
-            out.first = __builtin_amdgcn_readfirstlane(out.first);
-            out.end = __builtin_amdgcn_readfirstlane(out.end);
-            out.col_tile = (int)col_tile;
-            return true;
-        }
-        before += __shfl(upto, 63);
-    }
-    return false;
+__device__ __forceinline__ TilePlace tile_place(const TileTable& table, int experts, uint32_t row_tiles, uint32_t col_tiles,
+                                                uint32_t id) {
+    uint32_t row_tile, col_tile;
+    grouped_tile(id, row_tiles, col_tiles, row_tile, col_tile);
+    TilePlace out;
+    out.expert = expert_above(table.upto, experts, row_tile);
+    const uint32_t before = out.expert > 0 ? uniform(table.upto[out.expert - 1]) : 0;
+    out.first = uniform(table.begin[out.expert]) + (row_tile - before) * BM;
+    out.end = uniform(table.begin[out.expert + 1]);
+    out.col_tile = (int)col_tile;
+    return out;
 }
 
 // ---------------------------------------------------------------------------
@@ -485,10 +533,18 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall
     constexpr int kStages = DMA ? S::kStages : 2;
     __shared__ __attribute__((aligned(1024))) char tiles[kStages * S::kStage];
 
-    TilePlace place;
+    static_assert(sizeof(TileTable) <= sizeof(tiles), "the table lies where the tiles will");
+    TileTable& table = *reinterpret_cast<TileTable*>(tiles);
+    fill_tile_table(table, nullptr, a, [](int rows) { return ((uint32_t)rows + S::BM - 1) / S::BM; }, [](int) { return 0u; });
     const uint32_t col_tiles = ((uint32_t)a.cols_out + S::BN - 1) / S::BN;
-    if (!find_tile<S::BM>(a, first, launched, col_tiles, place))
+    const uint32_t row_tiles = uniform(table.upto[a.experts - 1]), all = row_tiles * col_tiles;
+    if (first >= all)
         return;
+    const uint32_t here = all - first < launched ? all - first : launched, in_run = die_order(blockIdx.x, here);
+    if (in_run >= here)
+        return;
+    const TilePlace place = tile_place<S::BM>(table, a.experts, row_tiles, col_tiles, first + in_run);
+    __syncthreads();
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int n0 = place.col_tile * S::BN, depth = a.cols_in, steps = (depth + kStep - 1) / kStep;
     const elem* const x = static_cast<const elem*>(a.x);
@@ -632,68 +688,6 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall
 // ---------------------------------------------------------------------------
 // The same in a run of tiles for each workgroup; rows of x and of the weights are made of aligned chunks.
 // ---------------------------------------------------------------------------
-struct TileTable {
-    int32_t upto[ZERO_ROUTE_MAX_EXPERTS];  // row tiles of the experts up to this one
-    int32_t lo[ZERO_ROUTE_MAX_EXPERTS], hi[ZERO_ROUTE_MAX_EXPERTS];
-};
-
-template <int BM>
-__device__ __forceinline__ void fill_tile_table(TileTable& table, const ExpertCall& a) {
-    const int lane = threadIdx.x & 63, slots = (int)a.slots;
-    if (threadIdx.x < 64) {
-        uint32_t before = 0;
-        for (int e0 = 0; e0 < a.experts; e0 += 64) {
-            const int e = e0 + lane;
-            int lo = 0, hi = 0;
-            if (e < a.experts) {
-                lo = a.offsets[e];
-                hi = a.offsets[e + 1];
-            }
-            lo = lo < 0 ? 0 : lo > slots ? slots : lo;
-            hi = hi < lo ? lo : hi > slots ? slots : hi;
-            uint32_t upto = ((uint32_t)(hi - lo) + BM - 1) / BM;
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const uint32_t o = __shfl_up(upto, d);
-                upto += lane >= d ? o : 0;
-            }
-            upto += before;
-            if (e < a.experts) {
-                table.upto[e] = (int)upto;
-                table.lo[e] = lo;
-                table.hi[e] = hi;
-            }
-            before = __shfl(upto, 63);
-        }
-    }
-    __syncthreads();
-}
-
-// Row tiles in groups of eight by all columns' tiles, whose operands a die's L2 serves.
-template <int BM>
-__device__ __forceinline__ TilePlace tile_place(const TileTable& table, int experts, uint32_t row_tiles, uint32_t col_tiles,
-                                                uint32_t id) {
-    constexpr uint32_t kGroup = 8;
-    const int lane = threadIdx.x & 63;
-    const uint32_t per = kGroup * col_tiles, group = id / per, rest = id - group * per;
-    const uint32_t rows_in = row_tiles - group * kGroup < kGroup ? row_tiles - group * kGroup : kGroup;
-    const uint32_t col_tile = rest / rows_in, row_tile = group * kGroup + rest - col_tile * rows_in;
-    TilePlace out{};
-    for (int e0 = 0; e0 < experts; e0 += 64) {
-        const int e = e0 + lane;
-        const uint64_t found = __ballot(e < experts && (uint32_t)table.upto[e < experts ? e : 0] > row_tile);
-        if (found) {
-            out.expert = e0 + __ffsll((unsigned long long)found) - 1;
-            break;
-        }
-    }
-    const uint32_t before = out.expert > 0 ? (uint32_t)table.upto[out.expert - 1] : 0;
-    out.first = __builtin_amdgcn_readfirstlane(table.lo[out.expert] + (int)((row_tile - before) * BM));
-    out.end = __builtin_amdgcn_readfirstlane(table.hi[out.expert]);
-    out.col_tile = (int)col_tile;
-    return out;
-}
-
 template <typename T, typename S, bool ALONG>
 __global__ __launch_bounds__(S::kThreads) void k_expert_product_run(const ExpertCall a) {
     using elem = typename T::elem;
@@ -708,9 +702,9 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product_run(const Expert
     __shared__ int32_t slots_of[kRing][S::BM];
     __shared__ TileTable table;
 
-    fill_tile_table<S::BM>(table, a);
+    fill_tile_table(table, nullptr, a, [](int rows) { return ((uint32_t)rows + S::BM - 1) / S::BM; }, [](int) { return 0u; });
     const uint32_t col_tiles = ((uint32_t)a.cols_out + S::BN - 1) / S::BN;
-    const uint32_t row_tiles = __builtin_amdgcn_readfirstlane(table.upto[a.experts - 1]), all = row_tiles * col_tiles;
+    const uint32_t row_tiles = uniform(table.upto[a.experts - 1]), all = row_tiles * col_tiles;
     // a die's workgroups take a run of the tiles in turn
     const uint32_t each = (all + 7) / 8, stride = gridDim.x / 8, die = blockIdx.x & 7;
     const uint32_t first = die * each + blockIdx.x / 8, last = (die + 1) * each < all ? (die + 1) * each : all;
@@ -791,11 +785,14 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product_run(const Expert
         ++copy_step;
         return true;
     };
+    // the first half of the weights' copies, x's, the others; across a half is half of the places
+    constexpr int kEarly = ALONG ? 0 : S::kColLoads / 2;
     auto copy = [&](int i, uint32_t stage) __attribute__((always_inline)) {
-        if (i < S::kRowLoads) {
+        if (i >= kEarly && i < kEarly + S::kRowLoads) {
+            i -= kEarly;
             copy_to_lds(k0 + xc < depth ? px[i] + k0 : zeros, stage + i * S::kThreads * 16);
         } else {
-            const int j = i - S::kRowLoads;
+            const int j = i < kEarly ? i : i - S::kRowLoads;
             const elem* from = pw;
             if constexpr (ALONG)
                 from += (w_room < j * kWRows ? w_room : j * kWRows) * a.ld_w + k0;
@@ -843,100 +840,109 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product_run(const Expert
             look_up(first + i * stride, i);
         wait_stage<0>();
     }
-    multiply_tiles<T, S>(tiles, lds_address(tiles) + wave * 1024, xs, ws, next_step, copy, tile_steps, finish);
+    multiply_tiles<T, S, kEarly>(tiles, lds_address(tiles) + wave * 1024, xs, ws, next_step, copy, tile_steps, finish);
 }
 
 // ---------------------------------------------------------------------------
-// dweight = x^T * dy, a tile of one expert's matrix for a workgroup, the expert's rows in `splits` parts
-// whose sums k_expert_join adds up.
+// dweight = x^T * dy, a tile of one expert's matrix for a workgroup.  An expert's rows are cut into parts of `part` rows;
+// where they are more than one, each leaves its sums in the workspace and k_expert_join adds them up.
 // ---------------------------------------------------------------------------
-template <typename T, typename S, bool DMA>
-__global__ __launch_bounds__(S::kThreads) void k_expert_weight_back(const ExpertCall a, uint32_t first,
-                                                                    uint32_t launched) {
+struct PartPlace {
+    int expert;
+    int begin, end;  // rows of the experts' order
+    uint32_t sums;   // which of the workspace's matrices it leaves its sums in
+    bool only;       // of its expert: it has the results themselves
+};
+
+__device__ __forceinline__ uint32_t parts_of(uint32_t rows, int part) {
+    return part == 0 || rows <= (uint32_t)part ? 1 : (rows + part - 1) / part;
+}
+
+__device__ __forceinline__ PartPlace part_place(const TileTable& table, const ExpertCall& a, uint32_t id) {
+    PartPlace p;
+    p.expert = expert_above(table.upto, a.experts, id);
+    const uint32_t nth = id - (p.expert > 0 ? uniform(table.upto[p.expert - 1]) : 0);
+    const int begin = uniform(table.begin[p.expert]), end = uniform(table.begin[p.expert + 1]);
+    const uint32_t all = parts_of(end - begin, a.part);
+    p.begin = begin + (int)nth * a.part;
+    p.end = nth + 1 == all ? end : p.begin + a.part;
+    p.sums = id;
+    p.only = all == 1;
+    return p;
+}
+
+// Where the results of a tile from (row, col) go.
+template <typename T, typename S>
+__device__ __forceinline__ void store_sums(const ExpertCall& a, const PartPlace& p, const f32x4 (&acc)[S::kTm][S::kTn], int row0,
+                                           int col, int lane) {
+    if (p.only) {
+        typename T::elem* const to = static_cast<typename T::elem*>(a.out) + (int64_t)p.expert * a.cols_in * a.ld_out;
+        store_tile<T, S, false>(acc, col, a.cols_out, lane, [&](int i) -> typename T::elem* {
+            return row0 + i < a.cols_in ? to + (row0 + i) * a.ld_out : nullptr;
+        });
+    } else {
+        float* const to = a.partial + (int64_t)p.sums * a.cols_in * a.cols_out;
+        store_tile<F32, S, false>(acc, col, a.cols_out, lane, [&](int i) -> float* {
+            return row0 + i < a.cols_in ? to + (int64_t)(row0 + i) * a.cols_out : nullptr;
+        });
+    }
+}
+
+// Operands of any alignment, through the registers; a workgroup a tile.
+template <typename T, typename S>
+__global__ __launch_bounds__(S::kThreads) void k_expert_weight_back(const ExpertCall a, uint32_t first, uint32_t launched) {
     using elem = typename T::elem;
     static_assert(S::BM == S::BN, "a thread's rows of x and dy are the same slots");
     constexpr int kPer = T::kPer, kStep = S::kBytes / (int)sizeof(elem);
     constexpr int kChunks = S::BN / kPer, kRows = S::kThreads / kChunks, kLoads = S::kColLoads;
-    constexpr int kStages = DMA ? S::kStages : 2, kAhead = kStages - 1;
-    static_assert(kStep <= 64, "a wave looks up a step's slots");
-    __shared__ __attribute__((aligned(1024))) char tiles[kStages * S::kStage];
-    constexpr int kRing = 2 * kStages;  // the steps that are looked up and not fetched yet, and more than a step between them
-    __shared__ int32_t slots_of[kRing][64];  // the steps' entries of order
+    __shared__ __attribute__((aligned(1024))) char tiles[2 * S::kStage];
+    static_assert(sizeof(TileTable) <= sizeof(tiles), "the table lies where the tiles will");
+    TileTable& table = *reinterpret_cast<TileTable*>(tiles);
 
-    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    fill_tile_table(table, nullptr, a, [&](int rows) { return parts_of(rows, a.part); }, [](int) { return 0u; });
     const uint32_t m_tiles = ((uint32_t)a.cols_in + S::BM - 1) / S::BM, n_tiles = ((uint32_t)a.cols_out + S::BN - 1) / S::BN;
-    uint32_t id = die_order(blockIdx.x, launched);
-    if (id >= launched)
+    const uint32_t of_part = m_tiles * n_tiles, all = uniform(table.upto[a.experts - 1]) * of_part;
+    if (first >= all)
         return;
-    id += first;
-    const uint32_t part = id / (m_tiles * n_tiles), tile = id - part * (m_tiles * n_tiles);
-    const int m0 = (int)(tile / n_tiles) * S::BM, n0 = (int)(tile % n_tiles) * S::BN;
-    const int expert = (int)(part / (uint32_t)a.splits), split = (int)(part % (uint32_t)a.splits);
-    const int slots = (int)a.slots;
-    int lo = __builtin_amdgcn_readfirstlane(a.offsets[expert]), hi = __builtin_amdgcn_readfirstlane(a.offsets[expert + 1]);
-    lo = lo < 0 ? 0 : lo > slots ? slots : lo;
-    hi = hi < lo ? lo : hi > slots ? slots : hi;
-    const int run = (int)(((uint32_t)(hi - lo) + kStep * a.splits - 1) / (kStep * a.splits)) * kStep;  // whole steps
-    const int64_t from = lo + (int64_t)run * split;
-    const int begin = from < hi ? (int)from : hi, end = hi - begin < run ? hi : begin + run;
-    const int steps = (end - begin + kStep - 1) / kStep;
+    const uint32_t here = all - first < launched ? all - first : launched, in_run = die_order(blockIdx.x, here);
+    if (in_run >= here)
+        return;
+    const uint32_t id = first + in_run;
+    const PartPlace place = part_place(table, a, id / of_part);
+    __syncthreads();
+    uint32_t m_tile, n_tile;
+    grouped_tile(id % of_part, m_tiles, n_tiles, m_tile, n_tile);
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int m0 = (int)m_tile * S::BM, n0 = (int)n_tile * S::BN;
+    const int steps = (int)(((uint32_t)(place.end - place.begin) + kStep - 1) / kStep);
     const elem* const x = static_cast<const elem*>(a.x);
     const elem* const dy = static_cast<const elem*>(a.w);
-    const elem* const zeros = reinterpret_cast<const elem*>(&zero_chunk);
 
-    int xc[kLoads], wc[kLoads];  // columns of this thread's chunks
-#pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-        const int c = ((t % kChunks) ^ across_exchange<T, kChunks>(t / kChunks + j * kRows)) * kPer;
-        xc[j] = m0 + c;
-        wc[j] = n0 + c;
-        if constexpr (DMA) {  // rows and columns past the last are not stored
-            xc[j] = xc[j] < a.cols_in ? xc[j] : a.cols_in - kPer;
-            wc[j] = wc[j] < a.cols_out ? wc[j] : a.cols_out - kPer;
-        }
-    }
-    const uint32_t lds = lds_address(tiles) + wave * 1024;
-    const bool ordered = a.x_map.mode | a.out_map.mode;
-    // A step's entries of order come to LDS with the tiles of the step kAhead before it.  (Loaded into registers they would
-    // have to be waited for, and with them, in the order of the loads, every copy that was issued before.)
-    // Each wave copies them all, to the same place.
-    auto look_up = [&](int step) __attribute__((always_inline)) {
-        const uint32_t i = (uint32_t)begin + (uint32_t)step * kStep + lane;  // may pass 2^31
-        if (ordered)
-            copy_word_to_lds(a.order + (i < (uint32_t)end ? i : end - 1), lds_address(slots_of[step % kRing]));
-    };
-    u32x4 rx[DMA ? 1 : kLoads], rw[DMA ? 1 : kLoads];
+    u32x4 rx[kLoads], rw[kLoads];
     auto fetch = [&](int step) __attribute__((always_inline)) {
-        const uint32_t stage = lds + step % kStages * S::kStage;
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             const int r = t / kChunks + j * kRows;
-            const int64_t i = begin + (int64_t)step * kStep + r;
-            const uint32_t slot = ordered ? slots_of[step % kRing][r] : 0;
-            const bool there = i < end && slot < (uint32_t)slots;
-            const elem* const px = x + (there ? (a.x_map.mode ? a.x_map.row(slot) : i) : 0) * a.ld_x;
-            const elem* const pw = dy + (there ? (a.out_map.mode ? a.out_map.row(slot) : i) : 0) * a.ld_w;
-            if constexpr (DMA) {
-                copy_to_lds(there ? px + xc[j] : zeros, stage + j * S::kThreads * 16);
-                copy_to_lds(there ? pw + wc[j] : zeros, stage + S::kRowsBytes + j * S::kThreads * 16);
-            } else {
-                rx[j] = rw[j] = u32x4{0, 0, 0, 0};
-                if (there) {
-                    rx[j] = load_row<T>(px, xc[j], a.cols_in, 0);
-                    rw[j] = load_row<T>(pw, wc[j], a.cols_out, 0);
-                }
-            }
+            const uint32_t i = (uint32_t)place.begin + (uint32_t)step * kStep + r;  // may pass 2^31
+            const int c = ((t % kChunks) ^ across_exchange<T, kChunks>(r)) * kPer;
+            rx[j] = rw[j] = u32x4{0, 0, 0, 0};
+            if (i >= (uint32_t)place.end)
+                continue;
+            const int64_t xr = row_at(a.order, a.x_map, a.slots, i), wr = row_at(a.order, a.out_map, a.slots, i);
+            if (xr < 0 || wr < 0)
+                continue;
+            if (m0 + c < a.cols_in)
+                rx[j] = load_row<T>(x + xr * a.ld_x, m0 + c, a.cols_in, 0);
+            if (n0 + c < a.cols_out)
+                rw[j] = load_row<T>(dy + wr * a.ld_w, n0 + c, a.cols_out, 0);
         }
-        look_up(step + kAhead);
     };
     auto put = [&](int step) __attribute__((always_inline)) {
-        if constexpr (!DMA) {
-            char* const stage = tiles + step % kStages * S::kStage + t * 16;
+        char* const stage = tiles + (step & 1) * S::kStage + t * 16;
 #pragma unroll
-            for (int j = 0; j < kLoads; ++j) {
-                *reinterpret_cast<u32x4*>(stage + j * S::kThreads * 16) = rx[j];
-                *reinterpret_cast<u32x4*>(stage + S::kRowsBytes + j * S::kThreads * 16) = rw[j];
-            }
+        for (int j = 0; j < kLoads; ++j) {
+            *reinterpret_cast<u32x4*>(stage + j * S::kThreads * 16) = rx[j];
+            *reinterpret_cast<u32x4*>(stage + S::kRowsBytes + j * S::kThreads * 16) = rw[j];
         }
     };
 
@@ -949,65 +955,216 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_weight_back(const Expert
 #pragma unroll
         for (int n = 0; n < S::kTn; ++n)
             acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-    // the copies of a step, its entries of order among them
-    constexpr int kCopies = DMA ? 2 * kLoads + 1 : 1;
     if (steps > 0) {
-        for (int s = 0; s < kAhead; ++s)
-            look_up(s);
-        wait_stage<0>();
+        fetch(0);
+        put(0);
     }
-    for (int s = 0; s < kAhead; ++s)
-        if (s < steps) {
-            fetch(s);
-            put(s);
-        }
     for (int s = 0; s < steps; ++s) {
-        // the last steps have nothing behind them; without an order there are fewer copies to wait for
-        if (kAhead > 1 && s + kAhead <= steps) {
-            if (ordered)
-                wait_stage<(kAhead - 1) * kCopies>();
-            else
-                wait_stage<(kAhead - 1) * (kCopies - 1)>();
-        } else {
-            wait_stage<0>();
-        }
-        if (s + kAhead < steps)
-            fetch(s + kAhead);
-        multiply<T, S>(tiles + s % kStages * S::kStage, xs, ws, acc);
-        if (s + kAhead < steps)
-            put(s + kAhead);
+        wait_stage<0>();
+        if (s + 1 < steps)
+            fetch(s + 1);
+        multiply<T, S>(tiles + (s & 1) * S::kStage, xs, ws, acc);
+        if (s + 1 < steps)
+            put(s + 1);
     }
+    store_sums<T, S>(a, place, acc, m0 + wm * S::kTm * 16, n0 + wn * S::kTn * 16, lane);
+}
 
-    const int col = n0 + wn * S::kTn * 16;
-    if (a.splits > 1) {
-        float* const p = a.partial + ((int64_t)split * a.experts + expert) * a.cols_in * a.cols_out;
-        store_tile<F32, S, false>(acc, col, a.cols_out, lane, [&](int m) -> float* {
-            const int row = m0 + wm * S::kTm * 16 + m;
-            return row < a.cols_in ? p + (int64_t)row * a.cols_out : nullptr;
-        });
-    } else {
-        elem* const p = static_cast<elem*>(a.out) + (int64_t)expert * a.cols_in * a.ld_out;
-        store_tile<T, S, false>(acc, col, a.cols_out, lane, [&](int m) -> elem* {
-            const int row = m0 + wm * S::kTm * 16 + m;
-            return row < a.cols_in ? p + row * a.ld_out : nullptr;
-        });
-    }
+// The same in a run of tiles for each workgroup; rows of x and dy are made of aligned chunks.
+template <typename T, typename S>
+__global__ __launch_bounds__(S::kThreads) void k_expert_weight_back_run(const ExpertCall a) {
+    using elem = typename T::elem;
+    static_assert(S::BM == S::BN, "a thread's rows of x and dy are the same slots");
+    constexpr int kPer = T::kPer, kStep = S::kBytes / (int)sizeof(elem);
+    constexpr int kChunks = S::BN / kPer, kRows = S::kThreads / kChunks, kLoads = S::kColLoads;
+    constexpr int kColumns = kRows % 16 == 0 ? 1 : 2;  // the exchange looks at four bits of the row
+    static_assert(kRows * kColumns % 16 == 0 && kLoads % (2 * kColumns) == 0 && kStep <= 64);
+    constexpr int kRing = 8;  // steps whose entries of order are held
+    static_assert(S::kStages == 2, "entries of order come two steps before the copies");
+    __shared__ __attribute__((aligned(1024))) char tiles[S::kStages * S::kStage];
+    __shared__ int32_t slots_of[kRing][64];
+    __shared__ TileTable table;
+
+    __shared__ uint32_t costs[ZERO_ROUTE_MAX_EXPERTS];
+    constexpr uint32_t kTileCost = 4;  // of a part's beginning and end, in steps
+    fill_tile_table(table, costs, a, [&](int rows) { return parts_of(rows, a.part); },
+                    [&](int rows) { return ((uint32_t)rows + kStep - 1) / kStep + kTileCost * parts_of(rows, a.part); });
+    const uint32_t m_tiles = ((uint32_t)a.cols_in + S::BM - 1) / S::BM, n_tiles = ((uint32_t)a.cols_out + S::BN - 1) / S::BN;
+    const uint32_t of_part = m_tiles * n_tiles, all = uniform(table.upto[a.experts - 1]) * of_part;
+    // A die's workgroups take a run of the tiles in turn, an eighth of the steps.
+    const uint32_t total = uniform(costs[a.experts - 1]);
+    auto die_begin = [&](uint32_t die) -> uint32_t {
+        if (die == 8)
+            return all;
+        const uint32_t at = (uint32_t)((uint64_t)total * die / 8);
+        const int e = expert_above(costs, a.experts, at);
+        const uint32_t before = e > 0 ? uniform(costs[e - 1]) : 0, own = uniform(costs[e]) - before;
+        const uint32_t part = e > 0 ? uniform(table.upto[e - 1]) : 0, parts = uniform(table.upto[e]) - part;
+        return part * of_part + (uint32_t)((uint64_t)(at - before) * (parts * of_part) / own);
+    };
+    const uint32_t stride = gridDim.x / 8, die = blockIdx.x & 7;
+    const uint32_t first = die_begin(die) + blockIdx.x / 8, last = die_begin(die + 1);
+    if (first >= last)
+        return;
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const uint32_t slots = (uint32_t)a.slots;
+    const elem* const zeros = reinterpret_cast<const elem*>(&zero_chunk);
+    const bool ordered = a.x_map.mode | a.out_map.mode;
+
+    // The steps of the tiles in turn.
+    struct Cursor {
+        uint32_t id;
+        int step, steps;
+        PartPlace place;
+    };
+    auto steps_of = [&](const PartPlace& p) __attribute__((always_inline)) -> int {
+        return (int)(((uint32_t)(p.end - p.begin) + kStep - 1) / kStep);
+    };
+    auto settle = [&](Cursor& c) __attribute__((always_inline)) {  // past tiles without steps
+        while (c.id < last) {
+            c.place = part_place(table, a, c.id / of_part);
+            c.steps = steps_of(c.place);
+            if (c.steps > 0)
+                return;
+            c.id += stride;
+        }
+    };
+    auto advance = [&](Cursor& c) __attribute__((always_inline)) {
+        if (++c.step == c.steps) {
+            c.step = 0;
+            c.id += stride;
+            settle(c);
+        }
+    };
+
+    // The entries of order come to LDS before the copies that need them.  (Loaded into registers they would have to be waited for,
+    // and with them, in the order of the loads, all copies issued before.)
+    Cursor look{first, 0, 0, {}};
+    settle(look);
+    int look_ring = 0;
+    auto look_up = [&](int by) __attribute__((always_inline)) {  // by wave `by`, or all
+        if (!ordered || look.id >= last)
+            return;
+        const uint32_t i = (uint32_t)look.place.begin + (uint32_t)look.step * kStep + lane;  // may pass 2^31
+        if (by < 0 || by == wave)
+            copy_word_to_lds(a.order + (i < (uint32_t)look.place.end ? i : look.place.end - 1), lds_address(slots_of[look_ring]));
+        look_ring = (look_ring + 1) % kRing;
+        advance(look);
+    };
+    for (int i = 0; i < 2 * S::kStages; ++i)
+        look_up(-1);
+    wait_stage<0>();
+
+    Cursor from{first, 0, 0, {}};
+    settle(from);
+    int ring = 0, turn = 0;
+    const elem *x = nullptr, *dy = nullptr;
+    const int cr = t / kChunks;
+    int xc[kColumns], wc[kColumns];  // columns of this thread's chunks
+    int rows_left = 0;
+    uint32_t base = 0;
+    uint32_t slot[kLoads];
+    uint32_t tile_now = ~0u;
+    auto next_step = [&]() __attribute__((always_inline)) -> bool {
+        if (from.id >= last)
+            return false;
+        if (from.id != tile_now) {
+            tile_now = from.id;
+            uint32_t m, n;
+            grouped_tile(from.id % of_part, m_tiles, n_tiles, m, n);
+#pragma unroll
+            for (int j = 0; j < kColumns; ++j) {  // rows and columns past the last are not stored
+                const int c = ((t % kChunks) ^ across_exchange<T, kChunks>(cr + j * kRows)) * kPer;
+                xc[j] = (int)m * S::BM + c;
+                wc[j] = (int)n * S::BN + c;
+                xc[j] = xc[j] < a.cols_in ? xc[j] : a.cols_in - kPer;
+                wc[j] = wc[j] < a.cols_out ? wc[j] : a.cols_out - kPer;
+            }
+        }
+        x = static_cast<const elem*>(a.x);
+        dy = static_cast<const elem*>(a.w);
+        base = (uint32_t)from.place.begin + (uint32_t)from.step * kStep;
+        rows_left = (int)((uint32_t)from.place.end - base);
+        if (ordered) {
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j)
+                slot[j] = (uint32_t)slots_of[ring][cr + j * kRows];
+            ring = (ring + 1) % kRing;
+        }
+        look_up(turn);
+        turn = turn + 1 == S::kThreads / 64 ? 0 : turn + 1;
+        advance(from);
+        return true;
+    };
+    // first the halves that are free sooner: x's and dy's first copies
+    constexpr int kHalf = kLoads / 2;
+    auto copy = [&](int i, uint32_t stage) __attribute__((always_inline)) {
+        const int half = i / (2 * kHalf), j = half * kHalf + i % kHalf;
+        const bool is_x = i % (2 * kHalf) < kHalf;
+        const int r = cr + j * kRows;
+        const bool there = r < rows_left && (!ordered || slot[j] < slots);
+        const SlotMap& map = is_x ? a.x_map : a.out_map;
+        const uint32_t row = map.mode == 0 ? base + r : (uint32_t)map.row(slot[j]);
+        const elem* p = is_x ? x + (int64_t)row * a.ld_x + xc[j % kColumns] : dy + (int64_t)row * a.ld_w + wc[j % kColumns];
+        copy_to_lds(there ? p : zeros, stage + (is_x ? 0 : S::kRowsBytes) + j * S::kThreads * 16);
+    };
+
+    uint32_t id = first;
+    bool begun = false;
+    auto tile_steps = [&]() __attribute__((always_inline)) -> int {
+        id += begun ? stride : 0;
+        begun = true;
+        return id < last ? steps_of(part_place(table, a, id / of_part)) : -1;
+    };
+    const int wm = wave % S::WM, wn = wave / S::WM;
+    const Side<T, false, false, S::BM, S::kTm, S::kBytes> xs(wm * S::kTm * 16, lane);
+    const Side<T, false, false, S::BN, S::kTn, S::kBytes> ws(wn * S::kTn * 16, lane);
+    auto finish = [&](f32x4 (&acc)[S::kTm][S::kTn]) __attribute__((always_inline)) {
+        uint32_t m, n;
+        grouped_tile(id % of_part, m_tiles, n_tiles, m, n);
+        store_sums<T, S>(a, part_place(table, a, id / of_part), acc, (int)m * S::BM + wm * S::kTm * 16,
+                         (int)n * S::BN + wn * S::kTn * 16, lane);
+    };
+    multiply_tiles<T, S, 2 * kHalf>(tiles, lds_address(tiles) + wave * 1024, xs, ws, next_step, copy, tile_steps, finish);
 }
 
 constexpr int kJoinBlock = 256;
 
-// dweight from the parts' sums, in the parts' order; a thread an element.
+// dweight of the experts of several parts from the parts' sums, in the parts' order; a thread four elements in turn, a row of
+// workgroups an expert.
 template <typename T>
-__global__ __launch_bounds__(kJoinBlock) void k_expert_join(const float* partial, int splits, int64_t all, int cols,
-                                                            typename T::elem* out, int64_t ld) {
-    const int64_t i = (int64_t)blockIdx.x * kJoinBlock + threadIdx.x;
+__global__ __launch_bounds__(kJoinBlock) void k_expert_join(const ExpertCall a) {
+    __shared__ TileTable table;
+    fill_tile_table(table, nullptr, a, [&](int rows) { return parts_of(rows, a.part); }, [](int) { return 0u; });
+    const int e = (int)blockIdx.y;
+    const uint32_t first = e > 0 ? table.upto[e - 1] : 0, last = table.upto[e];
+    if (last - first == 1)
+        return;
+    const int64_t all = (int64_t)a.cols_in * a.cols_out;
+    const int64_t i = ((int64_t)blockIdx.x * kJoinBlock + threadIdx.x) * 4;
     if (i >= all)
         return;
-    float sum = 0.f;
-    for (int s = 0; s < splits; ++s)
-        sum += partial[s * all + i];
-    out[i / cols * ld + i % cols] = T::of_f32(sum);
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    const float* const from = a.partial + first * all + i;
+    const int count = all - i < 4 ? (int)(all - i) : 4;
+    if (count == 4 && all % 4 == 0) {
+        for (uint32_t s = 0; s < last - first; ++s) {
+            float f[4];
+            F32::unpack(load_vec<F32, false>(from + s * all), f);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                sum[j] += f[j];
+        }
+    } else {
+        for (uint32_t s = 0; s < last - first; ++s)
+            for (int j = 0; j < count; ++j)
+                sum[j] += from[s * all + j];
+    }
+    typename T::elem* const out = static_cast<typename T::elem*>(a.out) + (int64_t)e * a.cols_in * a.ld_out;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (j < count)
+            out[(i + j) / a.cols_out * a.ld_out + (i + j) % a.cols_out] = T::of_f32(sum[j]);
 }
 
 // ---------------------------------------------------------------------------

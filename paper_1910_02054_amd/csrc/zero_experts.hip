@@ -2,6 +2,8 @@
 // (zero_expert_*): argument checks, choice of the kernels' shapes, launches.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
+
 #include "operator_args.hpp"
 #include "expert_kernels.hpp"
 
@@ -51,36 +53,33 @@ bool whole_chunks(const void* p, int64_t ld, int64_t cols, size_t elem) {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * elem % 16 == 0 && cols * elem % 16 == 0;
 }
 
-// The shape of the kernel that takes tiles in a run (operands in aligned chunks), by the experts' mean number of rows.
+constexpr int64_t kCus = 256;  // MI355X
+
+// The kernel that takes tiles in a run, in tiles of 256 or 128 rows by 256 columns: the shape whose rounds of tiles over the
+// compute units cost less.  A round of 128 rows is 0.58 of one of 256 (8192 slots of 16 experts 4096 to 1600 f16, 280 tiles in 2 rounds
+// of 256 or 504 in 2 of 128: 205 and 153 us; 4096 of 8 experts 1600 to 6400, 500 in 2 or 900 in 4: 109 and 122).
 template <typename F>
-int with_run_shape(int64_t mean, F f) {
-#ifndef ZO_MIN
-#define ZO_MIN 200
-#endif
-#ifndef ZO_ST
-#define ZO_ST 2
-#define ZO_KB 128
-#endif
-    if (mean <= ZO_MIN) return f(zo::TileShape<128, 256, 2, 4, ZO_ST, ZO_KB>{});
-    return f(zo::TileShape<256, 256, 2, 4, ZO_ST, ZO_KB>{});
+int with_run_shape(int64_t slots, int experts, int64_t cols_out, F f) {
+    auto rounds = [&](int64_t rows) {
+        return (double)div_up((slots / rows + experts / 2) * div_up(cols_out, 256), kCus);
+    };
+    if (0.58 * rounds(128) < rounds(256)) return f(zo::TileShape<128, 256, 2, 4, 3, 128>{});
+    return f(zo::TileShape<256, 256, 2, 4, 2, 128>{});
 }
 
-template <typename F>
-int with_product_shape(int64_t mean, F f) {
-    if (mean <= 48) return f(zo::TileShape<32, 128, 1, 4, 4, 128>{});
-    return f(zo::TileShape<128, 128, 2, 2, 2, 64>{});
+// Rows of a part of the weights' gradient's sums, 0: an expert's rows are one.  A longer part takes longer (1.5 us for 64
+// rows), a shorter one leaves more sums to be written and read again (at 4.5 TB/s): slots / part matrices of `size` floats.
+// The length at which both are the same, if the workspace's bound allows it.
+int64_t part_rows(int64_t slots, int experts, int64_t size) {
+    const int64_t room = ZERO_EXPERT_WORKSPACE_MAX / size - experts;  // parts behind each expert's first
+    if (room < 1)
+        return 0;
+    const double even = std::sqrt(8.0 * (double)size * (double)slots / 4.5e6 * 64 / 1.5);
+    const int64_t rows = std::max({(int64_t)256, (int64_t)even, div_up(slots, room)});
+    return rows < slots ? div_up(rows, 64) * 64 : 0;
 }
 
-// Parts of the summed axis in the weights' gradient: enough workgroups to fill the device twice, within the workspace's
-// bound, and of no less than 256 slots each on average.
-constexpr int kBackTile = 256;
-
-int back_splits(int64_t slots, int experts, int64_t cols_in, int64_t cols_out) {
-    const int64_t tiles = experts * div_up(cols_in, kBackTile) * div_up(cols_out, kBackTile);
-    const int64_t room = ZERO_EXPERT_WORKSPACE_MAX / std::max<int64_t>(1, experts * cols_in * cols_out);
-    return (int)std::max<int64_t>(1, std::min({div_up(512, tiles), room, slots / experts / 256}));
-}
-
+constexpr int64_t kFewRows = 48;  // of an expert on average: tiles of 32 rows
 constexpr uint32_t kMaxTiles = 1 << 20;  // workgroups of one launch
 
 }  // namespace
@@ -125,39 +124,41 @@ int zero_expert_product(const zero_expert_product_args_t* args, void* stream_) {
     c.experts = a.experts;
     c.cols_in = (int)a.cols_in;
     c.cols_out = (int)a.cols_out;
-    c.splits = 1;
     c.x_map = slot_map(a.x_slots);
     c.out_map = slot_map(a.y_slots);
     const bool dma = whole_chunks(a.x, a.ld_x, a.cols_in, e) && whole_chunks(a.weight, a.ld_weight, w_cols, e);
     return with_type(a.dtype, [&](auto type) {
         using T = decltype(type);
-        const int64_t mean = a.slots / a.experts;
-        if (dma && mean > 48)
-            return with_run_shape(mean, [&](auto shape) {
-                using S = decltype(shape);
-                const int64_t rows = std::min<int64_t>(a.slots, a.slots / S::BM + a.experts);
-                const int64_t tiles = rows * div_up(a.cols_out, S::BN);
-                const unsigned grid = (unsigned)std::min<int64_t>(256, div_up(tiles, 8) * 8);
-                auto* const kernel = a.transposed ? zo::k_expert_product_run<T, S, true> : zo::k_expert_product_run<T, S, false>;
-                kernel<<<grid, S::kThreads, 0, stream>>>(c);
-                HIP_TRY(hipGetLastError());
-                return ZERO_OK;
-            });
-        return with_product_shape(mean, [&](auto shape) {
+        auto by_tile = [&](auto shape, auto* kernel) {  // a workgroup a tile
             using S = decltype(shape);
             // every expert's last tile may hold one row
             const int64_t rows = std::min<int64_t>(a.slots, a.slots / S::BM + a.experts);
             const int64_t tiles = rows * div_up(a.cols_out, S::BN);
-            auto* const kernel = a.transposed ? (dma ? zo::k_expert_product<T, S, true, true>
-                                                     : zo::k_expert_product<T, S, true, false>)
-                                              : (dma ? zo::k_expert_product<T, S, false, true>
-                                                     : zo::k_expert_product<T, S, false, false>);
             for (int64_t first = 0; first < tiles; first += kMaxTiles) {
                 const uint32_t n = (uint32_t)std::min<int64_t>(kMaxTiles, tiles - first);
                 kernel<<<(n + 7) / 8 * 8, S::kThreads, 0, stream>>>(c, (uint32_t)first, n);
             }
             HIP_TRY(hipGetLastError());
-            return ZERO_OK;
+            return (int)ZERO_OK;
+        };
+        if (a.slots / a.experts <= kFewRows) {
+            using S = zo::TileShape<32, 128, 1, 4, 4, 128>;
+            return by_tile(S{}, a.transposed ? (dma ? zo::k_expert_product<T, S, true, true>
+                                                    : zo::k_expert_product<T, S, true, false>)
+                                             : (dma ? zo::k_expert_product<T, S, false, true>
+                                                    : zo::k_expert_product<T, S, false, false>));
+        }
+        if (!dma) {
+            using S = zo::TileShape<128, 128, 2, 2, 2, 64>;
+            return by_tile(S{}, a.transposed ? zo::k_expert_product<T, S, true, false>
+                                             : zo::k_expert_product<T, S, false, false>);
+        }
+        return with_run_shape(a.slots, a.experts, a.cols_out, [&](auto shape) {
+            using S = decltype(shape);
+            auto* const kernel = a.transposed ? zo::k_expert_product_run<T, S, true> : zo::k_expert_product_run<T, S, false>;
+            kernel<<<kCus, S::kThreads, 0, stream>>>(c);
+            HIP_TRY(hipGetLastError());
+            return (int)ZERO_OK;
         });
     });
 }
@@ -167,8 +168,8 @@ int zero_expert_workspace(int64_t slots, int32_t experts, int64_t cols_in, int64
     if (!floats)
         return fail(ZERO_EINVAL, "%s: NULL floats", fn);
     TRY(check_expert_sizes(fn, slots, experts, cols_in, cols_out));
-    const int splits = back_splits(slots, experts, cols_in, cols_out);
-    *floats = splits > 1 ? splits * experts * cols_in * cols_out : 0;
+    const int64_t rows = part_rows(slots, experts, cols_in * cols_out);
+    *floats = rows ? (slots / rows + experts) * cols_in * cols_out : 0;
     return ZERO_OK;
 }
 
@@ -211,30 +212,31 @@ int zero_expert_weight_backward(const zero_expert_weight_backward_args_t* args, 
     c.experts = a.experts;
     c.cols_in = (int)a.cols_in;
     c.cols_out = (int)a.cols_out;
-    c.splits = back_splits(a.slots, a.experts, a.cols_in, a.cols_out);
+    c.part = (int)part_rows(a.slots, a.experts, a.cols_in * a.cols_out);
     c.x_map = slot_map(a.x_slots);
     c.out_map = slot_map(a.dy_slots);
     const bool dma = whole_chunks(a.x, a.ld_x, a.cols_in, e) && whole_chunks(a.dy, a.ld_dy, a.cols_out, e);
     return with_type(a.dtype, [&](auto type) {
         using T = decltype(type);
-        auto launch = [&](auto shape) {
-            using S = decltype(shape);
-            const int64_t tiles = c.splits * a.experts * div_up(a.cols_in, S::BM) * div_up(a.cols_out, S::BN);
-            auto* const kernel = dma ? zo::k_expert_weight_back<T, S, true> : zo::k_expert_weight_back<T, S, false>;
+        if (dma) {
+            using S = zo::TileShape<256, 256, 2, 4, 2, 128>;
+            zo::k_expert_weight_back_run<T, S><<<kCus, S::kThreads, 0, stream>>>(c);
+        } else {
+            using S = zo::TileShape<128, 128, 2, 2, 2, 64>;
+            const int64_t parts = a.experts + (c.part ? a.slots / c.part : 0);
+            const int64_t tiles = parts * div_up(a.cols_in, S::BM) * div_up(a.cols_out, S::BN);
             for (int64_t first = 0; first < tiles; first += kMaxTiles) {
                 const uint32_t n = (uint32_t)std::min<int64_t>(kMaxTiles, tiles - first);
-                kernel<<<(n + 7) / 8 * 8, S::kThreads, 0, stream>>>(c, (uint32_t)first, n);
+                zo::k_expert_weight_back<T, S><<<(n + 7) / 8 * 8, S::kThreads, 0, stream>>>(c, (uint32_t)first, n);
             }
+        }
+        HIP_TRY(hipGetLastError());
+        if (c.part) {
+            const dim3 grid((unsigned)div_up(a.cols_in * a.cols_out, 4 * zo::kJoinBlock), (unsigned)a.experts);
+            zo::k_expert_join<T><<<grid, zo::kJoinBlock, 0, stream>>>(c);
             HIP_TRY(hipGetLastError());
-            if (c.splits > 1) {
-                const int64_t all = a.experts * a.cols_in * a.cols_out;
-                zo::k_expert_join<T><<<(unsigned)div_up(all, zo::kJoinBlock), zo::kJoinBlock, 0, stream>>>(
-                    c.partial, c.splits, all, (int)a.cols_out, static_cast<typename T::elem*>(a.dweight), a.ld_dweight);
-                HIP_TRY(hipGetLastError());
-            }
-            return ZERO_OK;
-        };
-        return launch(zo::TileShape<kBackTile, kBackTile, 2, 4, 4, 64>{});
+        }
+        return (int)ZERO_OK;
     });
 }
 
