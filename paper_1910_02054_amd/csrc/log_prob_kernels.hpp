@@ -7,11 +7,12 @@
 // every type: the maximum's own term is then 1 to the bit, so S >= 1, no log probability is above 0 and a
 // certain token has 0.
 //
-// The list: the threads' elements are kM groups, and the k-th largest of the groups' maxima is no more than
-// the k-th largest logit, so only logits from there on can be listed: little more than k of them unless
-// they lie close together in the row.  They are gathered in LDS and sorted by (logit, token).  Where they are
-// too many for that (rows of equal values, sorted rows, long lists), the k-th (logit, token) itself is
-// found, bit by bit, by counting.
+// The list: the threads' elements are groups (or their vectors are, for long lists), and the k-th largest of the groups'
+// maxima is no more than the k-th largest logit, so only logits from there on can be listed: little more than k of them
+// unless they lie close together in the row.  A bound just below it comes from a histogram of the maxima's distances from the
+// row's maximum; the threads whose own maximum is above it read their vectors again and queue those with such logits, which
+// a thread for each of their elements lists.  An entry's place is the number of entries above it.  Where too many are listed for that (rows of equal values), the k-th
+// (logit, token) itself is found, eight bits at a time.
 #pragma once
 
 #include "row_ops.hpp"
@@ -94,7 +95,7 @@ struct LogitRow {
             u = load_vec<T, false>(zv + n * kPer);
         return u;
     }
-    // f(vector, its first column), of all vectors; f(batch) before each batch's
+    // f(vector, its first column), of all vectors
     template <typename F>
     __device__ __forceinline__ void each(F f) {
         if constexpr (NV > 0) {
@@ -115,174 +116,197 @@ struct LogitRow {
             }
         }
     }
+    // the same, from memory
+    template <typename F>
+    __device__ __forceinline__ void each_again(F f) const {
+        constexpr int kAgain = 8;
+        for (int n0 = threadIdx.x; n0 < cut.vectors; n0 += kAgain * NT) {
+            u32x4 u[kAgain];
+#pragma unroll
+            for (int i = 0; i < kAgain; ++i)
+                u[i] = vector(n0 + i * NT);
+#pragma unroll
+            for (int i = 0; i < kAgain; ++i)
+                f(u[i], cut.head + (n0 + i * NT) * kPer);
+        }
+    }
 };
+
+constexpr int kDistanceBins = 512, kDigitBins = 256;
 
 template <int NT>
 struct LogProbLds {
     float wave_max[NT / 64], wave_sum[NT / 64], wave_u[NT / 64];
-    int32_t count[NT / 64];
-    uint32_t least;    // candidates' least key
-    int32_t listed;
+    __attribute__((aligned(16))) uint32_t bins[kDistanceBins];
+    uint32_t listed, queued;
 };
 
-// The sum over the workgroup of every wave's count; all threads call it together.
-template <int NT>
-__device__ __forceinline__ int sum_counts(int mine, LogProbLds<NT>& lds) {
-    mine = seg_reduce<64>(mine, [](int a, int b) { return a + b; });
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0)
-        lds.count[threadIdx.x / 64] = mine;
-    __syncthreads();
-    int all = 0;
-#pragma unroll
-    for (int w = 0; w < NT / 64; ++w)
-        all += lds.count[w];
-    return all;
+// The bin of a distance from the maximum, a sixteenth of an octave from 2^-12 to 2^20, those beyond in the first and the last.
+constexpr int kFirstBin = (127 - 12) << 4;
+__device__ __forceinline__ int distance_bin(float d) {
+    const int b = (int)(__builtin_bit_cast(uint32_t, d) >> 19) - kFirstBin;
+    return b < 0 ? 0 : b < kDistanceBins ? b : kDistanceBins - 1;
+}
+// The least distance that lies in no bin up to b.
+__device__ __forceinline__ float beyond_bin(int b) {
+    return b >= kDistanceBins - 1 ? __builtin_inff() : __builtin_bit_cast(float, (uint32_t)(b + 1 + kFirstBin) << 19);
 }
 
-// The likeliest k tokens of a row: `entries` ends with the sorted list in its first min(k, capacity) places,
-// 0 where there are none.  groups: the maximum of this thread's logits (-inf: none).
+// The first of COUNT bins (in the order of their number, or from the last down) up to which there are at least `want` entries,
+// -1: there are fewer.  before: entries in the bins before it, here: in it.  Every wave finds the same.
+template <int COUNT, bool DOWN>
+__device__ __forceinline__ int bin_reaching(const uint32_t* bins, uint32_t want, uint32_t& before, uint32_t& here) {
+    constexpr int kPer = COUNT / 64;
+    const int lane = threadIdx.x & 63;
+    uint32_t n[kPer], all = 0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        n[j] = bins[DOWN ? COUNT - 1 - (lane * kPer + j) : lane * kPer + j];
+        all += n[j];
+    }
+    uint32_t upto = all;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const uint32_t o = __shfl_up(upto, d);
+        upto += lane >= d ? o : 0;
+    }
+    const uint64_t reached = __ballot(upto >= want);
+    if (!reached)
+        return -1;
+    uint32_t sum = upto - all, mine = 0;
+    int at = -1;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        if (at < 0 && sum + n[j] >= want) {
+            at = lane * kPer + j;
+            mine = n[j];
+        }
+        sum += at < 0 ? n[j] : 0;
+    }
+    const int l = __ffsll((unsigned long long)reached) - 1;
+    before = __shfl(sum, l);
+    here = __shfl(mine, l);
+    at = __shfl(at, l);
+    return DOWN ? COUNT - 1 - at : at;
+}
+
+// One more in a bin, for the lanes that come here; lanes of a wave that mean the same bin add together.
+__device__ __forceinline__ void count_in(uint32_t* bins, int bin) {
+    const int first = __builtin_amdgcn_readfirstlane(bin);
+    const uint64_t here = __ballot(true);
+    if (__ballot(bin == first) == here) {
+        if ((threadIdx.x & 63) == __ffsll((unsigned long long)here) - 1)
+            atomicAdd(bins + first, (uint32_t)__popcll(here));
+    } else {
+        atomicAdd(bins + bin, 1u);
+    }
+}
+
+// The likeliest k tokens of a row, into `entries` in no order; returns how many.  most: the maximum of this
+// thread's logits, m: of the row's.  The bins are zero and no entry is listed.
 template <typename T, int NT, int NV>
-__device__ __forceinline__ void find_top(LogitRow<T, NT, NV>& row, float most, int k, int vocab, uint64_t* entries,
-                                         int capacity, LogProbLds<NT>& lds) {
-    const int t = threadIdx.x, lane = t & 63;
-    constexpr int kM = NT;  // groups: one a thread
-    uint32_t* const maxima = reinterpret_cast<uint32_t*>(entries);  // of the groups; capacity * 2 >= kM
-    uint32_t least = 1;
-    if (k <= kM / 2) {
-        maxima[t] = key_of(most);
-        if (t == 0)
-            lds.listed = 0;
-        __syncthreads();
-        if (t < 64) {
-            uint32_t mine[kM / 64];
-#pragma unroll
-            for (int j = 0; j < kM / 64; ++j)
-                mine[j] = maxima[j * 64 + lane];
-            uint32_t found = 0;
-            for (int b = 31; b >= 0; --b) {
-                const uint32_t next = found | 1u << b;
-                int n = 0;
-#pragma unroll
-                for (int j = 0; j < kM / 64; ++j)
-                    n += __popcll(__ballot(mine[j] >= next));
-                if (n >= k) {
-                    found = next;
-                    if (n <= k + k / 8 + 4)
-                        break;
-                }
-            }
-            if (lane == 0)
-                lds.least = found > 1 ? found : 1;
-        }
-        __syncthreads();
-        least = lds.least;
-        const float bound = of_key(least);
-        auto offer = [&](float f, int column) __attribute__((always_inline)) {
-            const uint32_t key = key_of(f);
-            if (key >= least && column < vocab) {
-                const int at = atomicAdd(&lds.listed, 1);
-                if (at < capacity)
-                    entries[at] = entry_of(key, column);
-            }
+__device__ __forceinline__ int find_top(const LogitRow<T, NT, NV>& row, const typename T::elem* z, float most, float m, int k,
+                                        uint64_t* entries, int capacity, LogProbLds<NT>& lds) {
+    const int t = threadIdx.x;
+    const float inf = __builtin_inff();
+    int32_t* const queue = reinterpret_cast<int32_t*>(entries + capacity);  // first columns of vectors
+    auto list = [&](float f, int token) __attribute__((always_inline)) {
+        const uint32_t at = atomicAdd(&lds.listed, 1u);
+        if (at < (uint32_t)capacity)
+            entries[at] = entry_of(key_of(f), token);
+    };
+    if (m == -inf)  // nothing but -inf and NaN
+        return 0;
+    int n = capacity + 1;
+    if (m < inf) {
+        auto add = [&](float f) __attribute__((always_inline)) {
+            if (f > -inf)
+                atomicAdd(lds.bins + distance_bin(m - f), 1u);
         };
-        (void)bound;
-        row.each([&](u32x4 u, int column) __attribute__((always_inline)) {
-            if (key_of(max_of<T>(u, -__builtin_inff())) >= least) {
-                float f[T::kPer];
-                T::unpack(u, f);
-#pragma unroll
-                for (int j = 0; j < T::kPer; ++j)
-                    offer(f[j], column + j);
-            }
-        });
-        if (t < row.cut.edges)
-            offer(row.edge, row.edge_column);
-        __syncthreads();
-    }
-    int n = k <= kM / 2 ? lds.listed : capacity + 1;
-    if (n > capacity) {
-        // the k-th entry itself: count of keys at least a bound, then of tokens at most one among the equal
-        auto count = [&](auto holds) __attribute__((always_inline)) {
-            int c = 0;
-            row.each([&](u32x4 u, int column) __attribute__((always_inline)) {
-                float f[T::kPer];
-                T::unpack(u, f);
-#pragma unroll
-                for (int j = 0; j < T::kPer; ++j)
-                    c += holds(key_of(f[j]), column + j) ? 1 : 0;
-            });
+        const bool by_thread = k <= NT / 4;
+        if (by_thread) {
+            add(most);
+        } else {
+            row.each_again([&](u32x4 u, int) __attribute__((always_inline)) { add(max_of<T>(u, -inf)); });
             if (t < row.cut.edges)
-                c += holds(key_of(row.edge), row.edge_column) ? 1 : 0;
-            return sum_counts<NT>(c, lds);
-        };
-        const int there = count([&](uint32_t key, int) { return key >= 1; });
-        const int want = there < k ? there : k;
-        uint32_t at = 1;  // the want-th largest key
-        if (want < there) {
-            at = 0;
-            for (int b = 31; b >= 0; --b) {
-                const uint32_t next = at | 1u << b;
-                if (count([&](uint32_t key, int) { return key >= next; }) >= want)
-                    at = next;
-            }
-        }
-        int last = vocab;  // tokens below it of the equal ones
-        if (want < there) {
-            const int above = count([&](uint32_t key, int) { return key > at; });
-            int low = 0;
-            for (int b = 30; b >= 0; --b) {
-                const int next = low | 1 << b;
-                if (next <= vocab &&
-                    count([&](uint32_t key, int token) { return key == at && token < next; }) < want - above)
-                    low = next;
-            }
-            last = low + 1;
+                add(row.edge);
         }
         __syncthreads();
-        if (t == 0)
-            lds.listed = 0;
-        __syncthreads();
-        auto take = [&](float f, int token) __attribute__((always_inline)) {
-            const uint32_t key = key_of(f);
-            if (key > at || (key == at && token < last))
-                if (key) {
-                    const int to = atomicAdd(&lds.listed, 1);
-                    if (to < capacity)
-                        entries[to] = entry_of(key, token);
+        uint32_t before = 0, here = 0;
+        const int bin = bin_reaching<kDistanceBins, false>(lds.bins, (uint32_t)k, before, here);
+        const float beyond = beyond_bin(bin < 0 ? kDistanceBins - 1 : bin);
+        auto counts = [&](float f) { return beyond < inf ? m - f < beyond : f > -inf; };
+        if (counts(most)) {
+            row.each_again([&](u32x4 u, int column) __attribute__((always_inline)) {
+                if (counts(max_of<T>(u, -inf))) {
+                    const uint32_t at = atomicAdd(&lds.queued, 1u);
+                    if (at < (uint32_t)capacity)
+                        queue[at] = column;
                 }
-        };
-        row.each([&](u32x4 u, int column) __attribute__((always_inline)) {
-            float f[T::kPer];
-            T::unpack(u, f);
-#pragma unroll
-            for (int j = 0; j < T::kPer; ++j)
-                take(f[j], column + j);
-        });
-        if (t < row.cut.edges)
-            take(row.edge, row.edge_column);
+            });
+            if (t < row.cut.edges && counts(row.edge))
+                list(row.edge, row.edge_column);
+        }
         __syncthreads();
-        n = lds.listed;
-    }
-    // sorted in falling order, 0 behind the last
-    int size = 64;
-    while (size < n || size < k)
-        size *= 2;
-    for (int i = n + t; i < size; i += NT)
-        entries[i] = 0;
-    __syncthreads();
-    for (int run = 2; run <= size; run *= 2)
-        for (int step = run / 2; step > 0; step /= 2) {
-            for (int i = t; i < size / 2; i += NT) {
-                const int p = 2 * i - (i & (step - 1)), q = p + step;
-                const uint64_t a = entries[p], b = entries[q];
-                if ((a < b) == ((p & run) == 0)) {
-                    entries[p] = b;
-                    entries[q] = a;
-                }
+        const int queued = (int)lds.queued;
+        if (queued <= capacity) {
+            for (int i = t; i < queued * T::kPer; i += NT) {
+                const int column = queue[i / T::kPer] + i % T::kPer;
+                const float f = T::to_f32(z[column]);
+                if (counts(f))
+                    list(f, column);
             }
             __syncthreads();
+            n = (int)lds.listed;
         }
+    }
+    if (n <= capacity)
+        return n;
+    // the k-th entry itself, from its highest digit down, or what is left of it where all entries with these digits are listed
+    auto each = [&](auto f) __attribute__((always_inline)) {
+        row.each_again([&](u32x4 u, int column) __attribute__((always_inline)) {
+            float v[T::kPer];
+            T::unpack(u, v);
+#pragma unroll
+            for (int j = 0; j < T::kPer; ++j)
+                if (v[j] > -inf)
+                    f(v[j], column + j);
+        });
+        if (t < row.cut.edges && row.edge > -inf)
+            f(row.edge, row.edge_column);
+    };
+    uint64_t bound = 0;
+    uint32_t want = (uint32_t)k;
+    for (int shift = 56; shift >= 0; shift -= 8) {
+        __syncthreads();
+        for (int i = t; i < kDigitBins; i += NT)
+            lds.bins[i] = 0;
+        __syncthreads();
+        each([&](float f, int token) __attribute__((always_inline)) {
+            const uint64_t e = entry_of(key_of(f), token) ^ bound;
+            if (shift == 56 || e >> (shift + 8 & 63) == 0)
+                count_in(lds.bins, (int)(e >> shift & 255));
+        });
+        __syncthreads();
+        uint32_t before = 0, here = 0;
+        const int digit = bin_reaching<kDigitBins, true>(lds.bins, want, before, here);
+        if (digit < 0)  // fewer than k in all
+            break;
+        want -= before;
+        bound |= (uint64_t)digit << shift;
+        if (here == want)
+            break;
+    }
+    __syncthreads();
+    if (t == 0)
+        lds.listed = 0;
+    __syncthreads();
+    each([&](float f, int token) __attribute__((always_inline)) {
+        if (entry_of(key_of(f), token) >= bound)
+            list(f, token);
+    });
+    __syncthreads();
+    return (int)lds.listed;
 }
 
 template <typename T, int NT, int NV, bool TOP>
@@ -295,6 +319,12 @@ __global__ __launch_bounds__(NT) void k_log_probs(const zero_log_probs_args_t a,
     const int t = threadIdx.x, wave = t / 64, lane = t & 63, vocab = (int)a.vocab;
     const float inf = __builtin_inff();
     const typename T::elem* const z = static_cast<const typename T::elem*>(a.logits) + at * a.ld_logits;
+    if constexpr (TOP) {
+        for (int i = t; i < kDistanceBins; i += NT)
+            lds.bins[i] = 0;
+        if (t == 0)
+            lds.listed = lds.queued = 0;
+    }
     int token = -1;
     float z_token = 0.f;
     if (a.logp && t == 0) {
@@ -370,12 +400,27 @@ __global__ __launch_bounds__(NT) void k_log_probs(const zero_log_probs_args_t a,
         }
     }
     if constexpr (TOP) {
-        find_top<T, NT, NV>(row, most, a.k, vocab, entries, capacity, lds);
-        for (int i = t; i < a.k; i += NT) {
-            const uint64_t e = entries[i];
-            const uint32_t key = (uint32_t)(e >> 32);
-            a.top_index[at * a.k + i] = key ? (int32_t)~(uint32_t)e : -1;
-            a.top_logp[at * a.k + i] = key ? log_p(of_key(key)) : -inf;
+        const int n = find_top<T, NT, NV>(row, z, most, m, a.k, entries, capacity, lds);
+        int32_t* const index = a.top_index + at * a.k;
+        float* const lp = a.top_logp + at * a.k;
+        // an entry's place is the number of those above it, counted by kShare threads
+        constexpr int kShare = 4;
+        for (int i0 = 0; i0 < n; i0 += NT / kShare) {
+            const int i = i0 + t / kShare, part = t % kShare;
+            const uint64_t e = entries[i < n ? i : n - 1];
+            int place = 0;
+#pragma unroll 8
+            for (int j = part; j < n; j += kShare)
+                place += entries[j] > e ? 1 : 0;
+            place = seg_reduce<kShare>(place, [](int p, int q) { return p + q; });
+            if (part == 0 && i < n && place < a.k) {
+                index[place] = (int32_t)~(uint32_t)e;
+                lp[place] = log_p(of_key((uint32_t)(e >> 32)));
+            }
+        }
+        for (int i = n + t; i < a.k; i += NT) {
+            index[i] = -1;
+            lp[i] = -inf;
         }
     }
 }
