@@ -226,14 +226,16 @@ __device__ __forceinline__ void wait_stage() {
 // there all waves meet, and step s + 1 has landed.  EARLY: copies of a stage that is free sooner, those of the columns'
 // first half where its rows are places of the axis; they begin kLead groups before the half's end, and the columns' second half
 // need not have landed before.  Copies 0 to EARLY - 1 are these, the last EARLY those of the second half.
-template <typename T, typename S, int EARLY, typename XS, typename WS, typename NEXT, typename COPY, typename STEPS,
-          typename FINISH>
-__device__ __forceinline__ void multiply_tiles(const char* tiles, uint32_t lds, const XS& xs, const WS& ws, NEXT next_step,
-                                               COPY copy, STEPS tile_steps, FINISH finish) {
+// Without DMA a step's copies go to registers a step earlier, and put(stage) writes them to LDS where all waves have met.
+template <typename T, typename S, bool DMA, int EARLY, typename XS, typename WS, typename NEXT, typename COPY, typename PUT,
+          typename STEPS, typename FINISH>
+__device__ __forceinline__ void multiply_tiles(char* tiles, uint32_t lds, const XS& xs, const WS& ws, NEXT next_step,
+                                               COPY copy, PUT put, STEPS tile_steps, FINISH finish) {
     constexpr int kLead = S::kTm / 2, kGroups = 2 * S::kTm;
     static_assert(S::kBytes == 128 && S::kTm % 2 == 0 && S::kTn % kLead == 0, "two halves, whole fragments a group");
     constexpr int kReads = S::kTn / kLead, kCopyRate = (S::kCopies - EARLY + kLead - 1) / kLead;
     constexpr int kEarlyRate = (EARLY + kLead - 1) / kLead;
+    static_assert(DMA || (EARLY == 0 && S::kStages == 2));
     bool more = false;
 #pragma unroll
     for (int s = 0; s < S::kStages; ++s) {
@@ -242,8 +244,17 @@ __device__ __forceinline__ void multiply_tiles(const char* tiles, uint32_t lds, 
 #pragma unroll
             for (int i = 0; i < S::kCopies; ++i)
                 copy(i, lds + s * S::kStage);
+        if (!DMA && more)
+            put(tiles + s * S::kStage);
     }
-    if (more)
+    if constexpr (!DMA) {
+        more = more && next_step();
+        if (more)
+#pragma unroll
+            for (int i = 0; i < S::kCopies; ++i)
+                copy(i, 0);
+    }
+    if (DMA && more)
         wait_stage<(S::kStages - 1) * S::kCopies + EARLY>();
     else
         wait_stage<0>();
@@ -277,10 +288,12 @@ __device__ __forceinline__ void multiply_tiles(const char* tiles, uint32_t lds, 
                     more = more && next_step();
                 }
                 if (q == kGroups - kLead) {
-                    if (more)
+                    if (DMA && more)
                         wait_stage<(S::kStages - 2) * S::kCopies + 2 * EARLY>();
                     else
                         wait_stage<0>();
+                    if (!DMA && more)
+                        put(tiles + at * S::kStage);
                     at = at + 1 == S::kStages ? 0 : at + 1;
                     from = tiles + at * S::kStage;
                     if (EARLY == 0)
@@ -688,7 +701,7 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall
 // ---------------------------------------------------------------------------
 // The same in a run of tiles for each workgroup; rows of x and of the weights are made of aligned chunks.
 // ---------------------------------------------------------------------------
-template <typename T, typename S, bool ALONG>
+template <typename T, typename S, bool ALONG, bool DMA>
 __global__ __launch_bounds__(S::kThreads) void k_expert_product_run(const ExpertCall a) {
     using elem = typename T::elem;
     constexpr int kPer = T::kPer, kStep = S::kBytes / (int)sizeof(elem);
@@ -763,20 +776,20 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product_run(const Expert
 #pragma unroll
             for (int j = 0; j < S::kRowLoads; ++j) {  // rows past the run's are not stored
                 const int64_t row = row_of(a.x_map, p, copy_ring, xr + j * kXRows);
-                px[j] = static_cast<const elem*>(a.x) + (row < 0 ? 0 : row) * a.ld_x + xc;  // none: stored as zeros
+                px[j] = static_cast<const elem*>(a.x) + (row < 0 ? 0 : row) * a.ld_x + (DMA ? xc : 0);  // none: stored as zeros
             }
             if constexpr (ALONG) {  // columns past the last are not stored
                 const int n = n0 + wr < a.cols_out ? n0 + wr : a.cols_out - 1;
-                pw = w + n * a.ld_w + wk;
+                pw = w + n * a.ld_w + (DMA ? wk : 0);
                 w_room = a.cols_out - 1 - n;
             } else {
                 pw = w + wr * a.ld_w;
 #pragma unroll
                 for (int j = 0; j < kColumns; ++j) {
                     const int c = n0 + ((t % kChunks) ^ across_exchange<T, kChunks>(wr + j * kWRows)) * kPer;
-                    wc[j] = c < a.cols_out ? c : a.cols_out - kPer;
+                    wc[j] = !DMA || c < a.cols_out ? c : a.cols_out - kPer;
                 }
-                if constexpr (kColumns == 1)
+                if constexpr (DMA && kColumns == 1)
                     pw += wc[0];
             }
             look_up(copy_id + S::kStages * stride, (copy_ring + S::kStages) % kRing);
@@ -786,22 +799,37 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product_run(const Expert
         return true;
     };
     // the first half of the weights' copies, x's, the others; across a half is half of the places
-    constexpr int kEarly = ALONG ? 0 : S::kColLoads / 2;
+    constexpr int kEarly = ALONG || !DMA ? 0 : S::kColLoads / 2;
+    u32x4 held[DMA ? 1 : S::kCopies];
     auto copy = [&](int i, uint32_t stage) __attribute__((always_inline)) {
         if (i >= kEarly && i < kEarly + S::kRowLoads) {
             i -= kEarly;
-            copy_to_lds(k0 + xc < depth ? px[i] + k0 : zeros, stage + i * S::kThreads * 16);
+            if constexpr (!DMA)
+                held[i] = load_row<T>(px[i], k0 + xc, depth, 0);
+            else
+                copy_to_lds(k0 + xc < depth ? px[i] + k0 : zeros, stage + i * S::kThreads * 16);
         } else {
             const int j = i < kEarly ? i : i - S::kRowLoads;
             const elem* from = pw;
             if constexpr (ALONG)
-                from += (w_room < j * kWRows ? w_room : j * kWRows) * a.ld_w + k0;
+                from += (w_room < j * kWRows ? w_room : j * kWRows) * a.ld_w + (DMA ? k0 : 0);
             else
-                from += (k0 + j * kWRows) * a.ld_w + (kColumns == 1 ? 0 : wc[j % kColumns]);
-            copy_to_lds(k0 + (ALONG ? 0 : j * kWRows) + wk < depth ? from : zeros, stage + S::kRowsBytes + j * S::kThreads * 16);
+                from += (k0 + j * kWRows) * a.ld_w + (DMA && kColumns > 1 ? wc[j % kColumns] : 0);
+            if constexpr (!DMA && ALONG)
+                held[i] = load_row<T>(from, k0 + wk, depth, 0);
+            else if constexpr (!DMA)
+                held[i] = load_row<T>(from, wc[j % kColumns], k0 + j * kWRows + wk < depth ? a.cols_out : 0, 0);
+            else
+                copy_to_lds(k0 + (ALONG ? 0 : j * kWRows) + wk < depth ? from : zeros, stage + S::kRowsBytes + j * S::kThreads * 16);
         }
     };
 
+    auto put = [&](char* stage) __attribute__((always_inline)) {
+        if constexpr (!DMA)
+#pragma unroll
+            for (int i = 0; i < S::kCopies; ++i)
+                *reinterpret_cast<u32x4*>(stage + (i * S::kThreads + t) * 16) = held[i];
+    };
     uint32_t id = first;
     int ring = 0;
     bool begun = false;
@@ -840,7 +868,7 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product_run(const Expert
             look_up(first + i * stride, i);
         wait_stage<0>();
     }
-    multiply_tiles<T, S, kEarly>(tiles, lds_address(tiles) + wave * 1024, xs, ws, next_step, copy, tile_steps, finish);
+    multiply_tiles<T, S, DMA, kEarly>(tiles, lds_address(tiles) + wave * 1024, xs, ws, next_step, copy, put, tile_steps, finish);
 }
 
 // ---------------------------------------------------------------------------
@@ -888,91 +916,9 @@ __device__ __forceinline__ void store_sums(const ExpertCall& a, const PartPlace&
     }
 }
 
-// Operands of any alignment, through the registers; a workgroup a tile.
-template <typename T, typename S>
-__global__ __launch_bounds__(S::kThreads) void k_expert_weight_back(const ExpertCall a, uint32_t first, uint32_t launched) {
-    using elem = typename T::elem;
-    static_assert(S::BM == S::BN, "a thread's rows of x and dy are the same slots");
-    constexpr int kPer = T::kPer, kStep = S::kBytes / (int)sizeof(elem);
-    constexpr int kChunks = S::BN / kPer, kRows = S::kThreads / kChunks, kLoads = S::kColLoads;
-    __shared__ __attribute__((aligned(1024))) char tiles[2 * S::kStage];
-    static_assert(sizeof(TileTable) <= sizeof(tiles), "the table lies where the tiles will");
-    TileTable& table = *reinterpret_cast<TileTable*>(tiles);
-
-    fill_tile_table(table, nullptr, a, [&](int rows) { return parts_of(rows, a.part); }, [](int) { return 0u; });
-    const uint32_t m_tiles = ((uint32_t)a.cols_in + S::BM - 1) / S::BM, n_tiles = ((uint32_t)a.cols_out + S::BN - 1) / S::BN;
-    const uint32_t of_part = m_tiles * n_tiles, all = uniform(table.upto[a.experts - 1]) * of_part;
-    if (first >= all)
-        return;
-    const uint32_t here = all - first < launched ? all - first : launched, in_run = die_order(blockIdx.x, here);
-    if (in_run >= here)
-        return;
-    const uint32_t id = first + in_run;
-    const PartPlace place = part_place(table, a, id / of_part);
-    __syncthreads();
-    uint32_t m_tile, n_tile;
-    grouped_tile(id % of_part, m_tiles, n_tiles, m_tile, n_tile);
-    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    const int m0 = (int)m_tile * S::BM, n0 = (int)n_tile * S::BN;
-    const int steps = (int)(((uint32_t)(place.end - place.begin) + kStep - 1) / kStep);
-    const elem* const x = static_cast<const elem*>(a.x);
-    const elem* const dy = static_cast<const elem*>(a.w);
-
-    u32x4 rx[kLoads], rw[kLoads];
-    auto fetch = [&](int step) __attribute__((always_inline)) {
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const int r = t / kChunks + j * kRows;
-            const uint32_t i = (uint32_t)place.begin + (uint32_t)step * kStep + r;  // may pass 2^31
-            const int c = ((t % kChunks) ^ across_exchange<T, kChunks>(r)) * kPer;
-            rx[j] = rw[j] = u32x4{0, 0, 0, 0};
-            if (i >= (uint32_t)place.end)
-                continue;
-            const int64_t xr = row_at(a.order, a.x_map, a.slots, i), wr = row_at(a.order, a.out_map, a.slots, i);
-            if (xr < 0 || wr < 0)
-                continue;
-            if (m0 + c < a.cols_in)
-                rx[j] = load_row<T>(x + xr * a.ld_x, m0 + c, a.cols_in, 0);
-            if (n0 + c < a.cols_out)
-                rw[j] = load_row<T>(dy + wr * a.ld_w, n0 + c, a.cols_out, 0);
-        }
-    };
-    auto put = [&](int step) __attribute__((always_inline)) {
-        char* const stage = tiles + (step & 1) * S::kStage + t * 16;
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            *reinterpret_cast<u32x4*>(stage + j * S::kThreads * 16) = rx[j];
-            *reinterpret_cast<u32x4*>(stage + S::kRowsBytes + j * S::kThreads * 16) = rw[j];
-        }
-    };
-
-    const int wm = wave % S::WM, wn = wave / S::WM;
-    const Side<T, false, false, S::BM, S::kTm, S::kBytes> xs(wm * S::kTm * 16, lane);
-    const Side<T, false, false, S::BN, S::kTn, S::kBytes> ws(wn * S::kTn * 16, lane);
-    f32x4 acc[S::kTm][S::kTn];
-#pragma unroll
-    for (int m = 0; m < S::kTm; ++m)
-#pragma unroll
-        for (int n = 0; n < S::kTn; ++n)
-            acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (steps > 0) {
-        fetch(0);
-        put(0);
-    }
-    for (int s = 0; s < steps; ++s) {
-        wait_stage<0>();
-        if (s + 1 < steps)
-            fetch(s + 1);
-        multiply<T, S>(tiles + (s & 1) * S::kStage, xs, ws, acc);
-        if (s + 1 < steps)
-            put(s + 1);
-    }
-    store_sums<T, S>(a, place, acc, m0 + wm * S::kTm * 16, n0 + wn * S::kTn * 16, lane);
-}
-
-// The same in a run of tiles for each workgroup; rows of x and dy are made of aligned chunks.
-template <typename T, typename S>
-__global__ __launch_bounds__(S::kThreads) void k_expert_weight_back_run(const ExpertCall a) {
+// DMA: rows of x and dy are made of aligned chunks, which go straight to LDS.
+template <typename T, typename S, bool DMA>
+__global__ __launch_bounds__(S::kThreads, 2) void k_expert_weight_back(const ExpertCall a) {
     using elem = typename T::elem;
     static_assert(S::BM == S::BN, "a thread's rows of x and dy are the same slots");
     constexpr int kPer = T::kPer, kStep = S::kBytes / (int)sizeof(elem);
@@ -1077,8 +1023,10 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_weight_back_run(const Ex
                 const int c = ((t % kChunks) ^ across_exchange<T, kChunks>(cr + j * kRows)) * kPer;
                 xc[j] = (int)m * S::BM + c;
                 wc[j] = (int)n * S::BN + c;
-                xc[j] = xc[j] < a.cols_in ? xc[j] : a.cols_in - kPer;
-                wc[j] = wc[j] < a.cols_out ? wc[j] : a.cols_out - kPer;
+                if constexpr (DMA) {
+                    xc[j] = xc[j] < a.cols_in ? xc[j] : a.cols_in - kPer;
+                    wc[j] = wc[j] < a.cols_out ? wc[j] : a.cols_out - kPer;
+                }
             }
         }
         x = static_cast<const elem*>(a.x);
@@ -1098,6 +1046,7 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_weight_back_run(const Ex
     };
     // first the halves that are free sooner: x's and dy's first copies
     constexpr int kHalf = kLoads / 2;
+    u32x4 held[DMA ? 1 : S::kCopies];
     auto copy = [&](int i, uint32_t stage) __attribute__((always_inline)) {
         const int half = i / (2 * kHalf), j = half * kHalf + i % kHalf;
         const bool is_x = i % (2 * kHalf) < kHalf;
@@ -1105,8 +1054,18 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_weight_back_run(const Ex
         const bool there = r < rows_left && (!ordered || slot[j] < slots);
         const SlotMap& map = is_x ? a.x_map : a.out_map;
         const uint32_t row = map.mode == 0 ? base + r : (uint32_t)map.row(slot[j]);
-        const elem* p = is_x ? x + (int64_t)row * a.ld_x + xc[j % kColumns] : dy + (int64_t)row * a.ld_w + wc[j % kColumns];
-        copy_to_lds(there ? p : zeros, stage + (is_x ? 0 : S::kRowsBytes) + j * S::kThreads * 16);
+        const elem* p = is_x ? x + (int64_t)row * a.ld_x : dy + (int64_t)row * a.ld_w;
+        const int c = is_x ? xc[j % kColumns] : wc[j % kColumns];
+        if constexpr (DMA)
+            copy_to_lds(there ? p + c : zeros, stage + (is_x ? 0 : S::kRowsBytes) + j * S::kThreads * 16);
+        else
+            held[is_x ? j : kLoads + j] = load_row<T>(p, c, there ? is_x ? a.cols_in : a.cols_out : 0, 0);
+    };
+    auto put = [&](char* stage) __attribute__((always_inline)) {
+        if constexpr (!DMA)
+#pragma unroll
+            for (int i = 0; i < S::kCopies; ++i)
+                *reinterpret_cast<u32x4*>(stage + (i * S::kThreads + t) * 16) = held[i];
     };
 
     uint32_t id = first;
@@ -1125,7 +1084,8 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_weight_back_run(const Ex
         store_sums<T, S>(a, part_place(table, a, id / of_part), acc, (int)m * S::BM + wm * S::kTm * 16,
                          (int)n * S::BN + wn * S::kTn * 16, lane);
     };
-    multiply_tiles<T, S, 2 * kHalf>(tiles, lds_address(tiles) + wave * 1024, xs, ws, next_step, copy, tile_steps, finish);
+    multiply_tiles<T, S, DMA, DMA ? 2 * kHalf : 0>(tiles, lds_address(tiles) + wave * 1024, xs, ws, next_step, copy, put,
+                                                   tile_steps, finish);
 }
 
 constexpr int kJoinBlock = 256;

@@ -148,17 +148,21 @@ int zero_expert_product(const zero_expert_product_args_t* args, void* stream_) {
                                              : (dma ? zo::k_expert_product<T, S, false, true>
                                                     : zo::k_expert_product<T, S, false, false>));
         }
-        if (!dma) {
-            using S = zo::TileShape<128, 128, 2, 2, 2, 64>;
-            return by_tile(S{}, a.transposed ? zo::k_expert_product<T, S, true, false>
-                                             : zo::k_expert_product<T, S, false, false>);
-        }
-        return with_run_shape(a.slots, a.experts, a.cols_out, [&](auto shape) {
+        auto in_runs = [&](auto shape, auto* kernel) {
             using S = decltype(shape);
-            auto* const kernel = a.transposed ? zo::k_expert_product_run<T, S, true> : zo::k_expert_product_run<T, S, false>;
             kernel<<<kCus, S::kThreads, 0, stream>>>(c);
             HIP_TRY(hipGetLastError());
             return (int)ZERO_OK;
+        };
+        if (!dma) {
+            using S = zo::TileShape<128, 256, 2, 4, 2, 128>;
+            return in_runs(S{}, a.transposed ? zo::k_expert_product_run<T, S, true, false>
+                                             : zo::k_expert_product_run<T, S, false, false>);
+        }
+        return with_run_shape(a.slots, a.experts, a.cols_out, [&](auto shape) {
+            using S = decltype(shape);
+            return in_runs(shape, a.transposed ? zo::k_expert_product_run<T, S, true, true>
+                                               : zo::k_expert_product_run<T, S, false, true>);
         });
     });
 }
@@ -220,15 +224,10 @@ int zero_expert_weight_backward(const zero_expert_weight_backward_args_t* args, 
         using T = decltype(type);
         if (dma) {
             using S = zo::TileShape<256, 256, 2, 4, 2, 128>;
-            zo::k_expert_weight_back_run<T, S><<<kCus, S::kThreads, 0, stream>>>(c);
+            zo::k_expert_weight_back<T, S, true><<<kCus, S::kThreads, 0, stream>>>(c);
         } else {
-            using S = zo::TileShape<128, 128, 2, 2, 2, 64>;
-            const int64_t parts = a.experts + (c.part ? a.slots / c.part : 0);
-            const int64_t tiles = parts * div_up(a.cols_in, S::BM) * div_up(a.cols_out, S::BN);
-            for (int64_t first = 0; first < tiles; first += kMaxTiles) {
-                const uint32_t n = (uint32_t)std::min<int64_t>(kMaxTiles, tiles - first);
-                zo::k_expert_weight_back<T, S><<<(n + 7) / 8 * 8, S::kThreads, 0, stream>>>(c, (uint32_t)first, n);
-            }
+            using S = zo::TileShape<128, 128, 2, 2, 2, 128>;  // two workgroups to a compute unit
+            zo::k_expert_weight_back<T, S, false><<<2 * kCus, S::kThreads, 0, stream>>>(c);
         }
         HIP_TRY(hipGetLastError());
         if (c.part) {
