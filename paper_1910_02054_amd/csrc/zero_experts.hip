@@ -150,10 +150,19 @@ int zero_expert_product(const zero_expert_product_args_t* args, void* stream_) {
         }
         auto in_runs = [&](auto shape, auto* kernel) {
             using S = decltype(shape);
-            kernel<<<kCus, S::kThreads, 0, stream>>>(c);
+            kernel<<<kCus * 512 / S::kThreads, S::kThreads, 0, stream>>>(c);
             HIP_TRY(hipGetLastError());
             return (int)ZERO_OK;
         };
+        // fp32: the products take most of the time whatever the tile (a sixteenth of bf16's rate), so small tiles, evenly over the
+        // compute units (3063 slots of 12 experts 803 to 1203: 117 us, 201 in tiles of 128 by 128, 167 of 128 by 256)
+        if constexpr (T::kPer == 4) {
+            using S = zo::TileShape<64, 128, 2, 2, 2, 128>;
+            return in_runs(S{}, a.transposed ? (dma ? zo::k_expert_product_run<T, S, true, true>
+                                                    : zo::k_expert_product_run<T, S, true, false>)
+                                             : (dma ? zo::k_expert_product_run<T, S, false, true>
+                                                    : zo::k_expert_product_run<T, S, false, false>));
+        }
         if (!dma) {
             using S = zo::TileShape<128, 256, 2, 4, 2, 128>;
             return in_runs(S{}, a.transposed ? zo::k_expert_product_run<T, S, true, false>
@@ -222,13 +231,16 @@ int zero_expert_weight_backward(const zero_expert_weight_backward_args_t* args, 
     const bool dma = whole_chunks(a.x, a.ld_x, a.cols_in, e) && whole_chunks(a.dy, a.ld_dy, a.cols_out, e);
     return with_type(a.dtype, [&](auto type) {
         using T = decltype(type);
-        if (dma) {
-            using S = zo::TileShape<256, 256, 2, 4, 2, 128>;
-            zo::k_expert_weight_back<T, S, true><<<kCus, S::kThreads, 0, stream>>>(c);
-        } else {
-            using S = zo::TileShape<128, 128, 2, 2, 2, 128>;  // two workgroups to a compute unit
-            zo::k_expert_weight_back<T, S, false><<<2 * kCus, S::kThreads, 0, stream>>>(c);
-        }
+        // Tiles of 256 by 256, but where they would be half empty (16384 slots of 64 experts, 128 by 128 f16: 21 us, 27 in tiles of 256;
+        // 65536 of 64, 512 by 256 bf16: 80 and 62) and for fp32, bound by the products (8192 of 8, 1024 by 4096: 835 and 1138).
+        using Wide = zo::TileShape<256, 256, 2, 4, 2, 128>;
+        using Small = zo::TileShape<128, 128, 2, 2, 2, 128>;  // two workgroups to a compute unit
+        if (!dma)
+            zo::k_expert_weight_back<T, Small, false><<<2 * kCus, Small::kThreads, 0, stream>>>(c);
+        else if (T::kPer == 4 || std::min(a.cols_in, a.cols_out) <= 128)
+            zo::k_expert_weight_back<T, Small, true><<<2 * kCus, Small::kThreads, 0, stream>>>(c);
+        else if constexpr (T::kPer == 8)
+            zo::k_expert_weight_back<T, Wide, true><<<kCus, Wide::kThreads, 0, stream>>>(c);
         HIP_TRY(hipGetLastError());
         if (c.part) {
             const dim3 grid((unsigned)div_up(a.cols_in * a.cols_out, 4 * zo::kJoinBlock), (unsigned)a.experts);
