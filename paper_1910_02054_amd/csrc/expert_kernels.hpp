@@ -1,15 +1,17 @@
 // expert_kernels.hpp -- products of the experts' rows with their weights, and the weights'
 // gradient: tiles of both operands in LDS, sums in the matrix cores' registers.
 //
-// A step of the sum takes 64 or 128 bytes of its axis (32 or 64 elements of 16 bits).  An operand's tile
+// A step of the sum takes 128 bytes of its axis (64 elements of 16 bits, 32 of fp32).  An operand's tile
 // comes in one of two layouts, as it lies in memory:
-//   along    its rows run along the summed axis (x; weights that lie [out, in]): tile rows of a step's bytes
+//   along    its rows run along the summed axis (x; weights that lie [out, in]): tile rows of 128 bytes
 //   across   they run across it (weights that lie [in, out]; both operands of the gradient): one
 //            tile row for each place of the axis, which the matrix instruction wants transposed;
 //            ds_read_b64_tr_b16 does that for 16 bits, fp32's fragments are single words anyway
-// The 16-byte chunks of a tile row are exchanged by a few bits of the row, so that the lanes of a fragment
-// read different banks; the copy to LDS writes chunks in the lanes' order, so the exchange is in the address
-// that a lane reads from memory.
+// The 16-byte chunks of a tile row are exchanged by a few bits of the row, so that the lanes of a fragment read
+// different banks; the copy to LDS writes chunks in the lanes' order, so the exchange is in the address that a
+// lane reads from memory.  (A ds_read_b128 takes lanes 0 to 3, 12 to 15 and 20 to 27 in one cycle, 4 to 11, 16 to
+// 19 and 28 to 31 in the next, and likewise the upper half; the exchanges keep those apart, and the counters show
+// no conflict.)
 //
 // The first operand of a matrix instruction is the columns' side (weights, dy), the second the rows' (x):
 // a lane then holds neighbouring columns of one row of the result.
@@ -29,6 +31,8 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef u32x2 u32x2_e2 __attribute__((aligned(2)));
+
+constexpr int kStepBytes = 128;  // of the summed axis
 
 // The rows of a matrix (ZERO's `*_slots`): `mode` 0, 1 or n; a slot's row for n is slot * mul >> shift.
 struct SlotMap {
@@ -89,14 +93,12 @@ __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
     }
 }
 
-// Along: the exchange of the chunks of tile row r, rows of BYTES.  On the columns' side a pair of fragments takes 32 rows so
-// that a lane's 4 + 4 results are neighbours: fragment f, lane row a is tile row 32 (f / 2) + 8 (a / 4) + 4 (f % 2) + a % 4.
-template <bool PAIRED, int BYTES>
+// Along: the exchange of the chunks of tile row r.  On the columns' side a pair of fragments takes 32 rows so that
+// a lane's 4 + 4 results are neighbours: fragment f, lane row a is tile row 32 (f / 2) + 8 (a / 4) + 4 (f % 2) + a
+// % 4.
+template <bool PAIRED>
 __device__ __forceinline__ int along_exchange(int r) {
-    if constexpr (BYTES == 128)
-        return PAIRED ? (r & 3) | (r >> 3 & 1) << 2 : r & 7;
-    else
-        return (r >> (PAIRED ? 4 : 3) & 1) * 3;
+    return PAIRED ? (r & 3) | (r >> 3 & 1) << 2 : r & 7;
 }
 
 // Across: the exchange of the chunks of the tile row of place k, for rows of CHUNKS chunks.
@@ -109,20 +111,19 @@ __device__ __forceinline__ int across_exchange(int k) {
 }
 
 // One side of a wave's fragments: byte offsets in the tile, once for each fragment or half step.
-template <typename T, bool ALONG, bool PAIRED, int TILE, int COUNT, int BYTES>
+template <typename T, bool ALONG, bool PAIRED, int TILE, int COUNT>
 struct Side {
-    static constexpr int kRow = ALONG ? BYTES : TILE * (int)sizeof(typename T::elem);  // bytes of a tile row
+    static constexpr int kRow = ALONG ? kStepBytes : TILE * (int)sizeof(typename T::elem);  // bytes of a tile row
     static constexpr int kChunks = kRow / 16;
-    static constexpr int kReads = ALONG ? 1 : T::kPer == 4 ? 4 : 2;  // of a fragment
-    int at[ALONG ? BYTES / 64 : COUNT];
+    int at[ALONG ? 2 : COUNT];
     // first: the wave's first row (along) or column (across) in the tile
     __device__ __forceinline__ Side(int first, int lane) {
         const int a = lane & 15, g = lane >> 4;
         if constexpr (ALONG) {
             const int r = first + (PAIRED ? 8 * (a >> 2) + (a & 3) : a);
-            const int c = g ^ along_exchange<PAIRED, BYTES>(r);
+            const int c = g ^ along_exchange<PAIRED>(r);
 #pragma unroll
-            for (int kk = 0; kk < BYTES / 64; ++kk)
+            for (int kk = 0; kk < 2; ++kk)
                 at[kk] = r * kRow + (c ^ 4 * kk) * 16;
         } else if constexpr (T::kPer == 4) {
 #pragma unroll
@@ -159,14 +160,15 @@ struct Side {
     }
 };
 
-// BYTES of the summed axis a step.
-template <int BM_, int BN_, int WM_, int WN_, int STAGES_, int BYTES_>
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
 struct TileShape {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kStages = STAGES_, kBytes = BYTES_;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kStages = STAGES_;
     static constexpr int kThreads = 64 * WM * WN, kTm = BM / WM / 16, kTn = BN / WN / 16;
-    static constexpr int kRowsBytes = BM * kBytes, kColsBytes = BN * kBytes, kStage = kRowsBytes + kColsBytes;
+    static constexpr int kRowsBytes = BM * kStepBytes, kColsBytes = BN * kStepBytes, kStage = kRowsBytes + kColsBytes;
     static constexpr int kRowLoads = kRowsBytes / 16 / kThreads, kColLoads = kColsBytes / 16 / kThreads;  // a thread's
     static constexpr int kCopies = kRowLoads + kColLoads;
+    static constexpr int kPerCu = kStages * kStage > 80 * 1024 ? 1 : 2;  // workgroups, by their LDS
+    static constexpr int kWaves = kPerCu * WM * WN / 4;                  // of a SIMD
     static_assert(kRowLoads * 16 * kThreads == kRowsBytes && kColLoads * 16 * kThreads == kColsBytes, "whole loads");
 };
 
@@ -174,7 +176,7 @@ struct TileShape {
 template <typename T, typename S, typename XS, typename WS>
 __device__ __forceinline__ void multiply(const char* stage, const XS& xs, const WS& ws, f32x4 (&acc)[S::kTm][S::kTn]) {
 #pragma unroll
-    for (int kk = 0; kk < S::kBytes / 64; ++kk) {
+    for (int kk = 0; kk < 2; ++kk) {
         u32x4 xf[S::kTm], wf[S::kTn];
 #pragma unroll
         for (int n = 0; n < S::kTn; ++n)
@@ -190,16 +192,17 @@ __device__ __forceinline__ void multiply(const char* stage, const XS& xs, const 
     }
 }
 
-// 16 bytes straight to LDS: lane l's land at base + 16 l.  Written as an instruction because the compiler holds every
-// ds_read_tr behind all copies that it knows of (s_waitcnt vmcnt(0) before the step's first fragment: 16384 x 8 slots
-// 1024 to 4096 bf16 1612 us); wait_stage has the waits.  There is no output register, and nothing else in these kernels uses m0.
+// 16 bytes straight to LDS: lane l's land at base + 16 l.  Written as an instruction because the compiler holds
+// every ds_read_tr behind all copies that it knows of (s_waitcnt vmcnt(0) before the step's first fragment: of the
+// simplest kernel 16384 x 8 slots 1024 to 4096 bf16 took 1612 us, 1300 with this); wait_stage has the waits.
+// There is no output register.
 __device__ __forceinline__ void copy_to_lds(const void* from, uint32_t base) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(base), "v"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(base), "v"(from) : "memory", "m0");
 }
 
 // 4 bytes, lane l's to base + 4 l.
 __device__ __forceinline__ void copy_word_to_lds(const void* from, uint32_t base) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(base), "v"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(base), "v"(from) : "memory", "m0");
 }
 
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)ZO_LDS(const void, p); }
@@ -215,24 +218,33 @@ __device__ __forceinline__ void wait_stage() {
     asm volatile("" ::: "memory");
 }
 
-// The tiles that a workgroup takes, one after another, as one run of steps: the copies of a tile's first steps are under way
-// before the tile before it has ended, and its results are stored while they land.
+// The tiles that a workgroup takes, one after another, as one run of steps: the copies of a tile's first steps are
+// under way before the tile before it has ended, and its results are stored while they land.
 //   next_step()          prepares the copies of the run's next step; false: there is none
 //   copy(i, stage)       issues copy i of that step, into the stage at LDS address `stage`
 //   tile_steps()         the steps of the next tile, below 0: none
 //   finish(acc)          stores a tile's results
-// A step is two halves of kTm groups of products, one of the rows' fragments with all of the columns'.  Fragments are read
-// kLead groups before they are needed, so kLead groups before a step's end its stage is free for the copies of step s + kStages:
-// there all waves meet, and step s + 1 has landed.  EARLY: copies of a stage that is free sooner, those of the columns'
-// first half where its rows are places of the axis; they begin kLead groups before the half's end, and the columns' second half
-// need not have landed before.  Copies 0 to EARLY - 1 are these, the last EARLY those of the second half.
-// Without DMA a step's copies go to registers a step earlier, and put(stage) writes them to LDS where all waves have met.
+// A step is two halves of kTm groups of products, one of the rows' fragments with all of the columns'.  Fragments
+// are read kLead groups before they are needed, so kLead groups before a step's end its stage is free for the
+// copies of step s + kStages: there all waves meet, and step s + 1 has landed.  EARLY: copies of a stage that is
+// free sooner, those of the columns' first half where its rows are places of the axis; they begin kLead groups
+// before the half's end, and the columns' second half need not have landed before.  Copies 0 to EARLY - 1 are
+// these, the last EARLY those of the second half. Without DMA a step's copies go to registers a step earlier, and
+// put(stage) writes them to LDS where all waves have met.
+//
+// What bounds it, 16384 x 8 slots 1024 to 4096 bf16 (1140 us, 964 TFLOP/s; batched library products of equal sizes
+// 1086): the products with their fragments' reads alone 733 us, as fast as the library's 8192^3; the copies alone
+// 547; both 985 to 1020, since LDS serves reads and copies by turns and a step's copies have a step's time to
+// land; the stores the rest.  In steps taken: a workgroup a tile 1300; tiles in a run 1245; whole lines stored
+// 1186; the early halves 1146.  Tried and left: steps of 64 bytes in four stages (half lines copied: 1315), lines
+// touched ahead for L2 (1229), four waves of 128 by 128 (2830: one wave a SIMD), stores past the caches, a raised
+// wave priority and groups of 4 or 16 row tiles (no difference).
 template <typename T, typename S, bool DMA, int EARLY, typename XS, typename WS, typename NEXT, typename COPY, typename PUT,
           typename STEPS, typename FINISH>
 __device__ __forceinline__ void multiply_tiles(char* tiles, uint32_t lds, const XS& xs, const WS& ws, NEXT next_step,
                                                COPY copy, PUT put, STEPS tile_steps, FINISH finish) {
     constexpr int kLead = S::kTm / 2, kGroups = 2 * S::kTm;
-    static_assert(S::kBytes == 128 && S::kTm % 2 == 0 && S::kTn % kLead == 0, "two halves, whole fragments a group");
+    static_assert(S::kTm % 2 == 0 && S::kTn % kLead == 0, "two halves, whole fragments a group");
     constexpr int kReads = S::kTn / kLead, kCopyRate = (S::kCopies - EARLY + kLead - 1) / kLead;
     constexpr int kEarlyRate = (EARLY + kLead - 1) / kLead;
     static_assert(DMA || (EARLY == 0 && S::kStages == 2));
@@ -356,9 +368,10 @@ __device__ __forceinline__ uint32_t from_other_half(uint32_t x) {
     return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xF, 0xF, true);  // row_ror:8
 }
 
-// A wave's results: out(m) is the row of its m-th (null: none), `first` its first column.  A lane has some columns of row
-// l % 16.  Where 128 bytes of all rows exist they are stored as whole lines, eight lanes to a line: the lanes of
-// rows r and r + 8 exchange halves of their lines.  (Stored as they are, 32 bytes at a time: 131072 rows of 4096 bf16 240 us.)
+// A wave's results: out(m) is the row of its m-th (null: none), `first` its first column.  A lane has some columns
+// of row l % 16.  Where 128 bytes of all rows exist they are stored as whole lines, eight lanes to a line: the
+// lanes of rows r and r + 8 exchange halves of their lines (stored 32 bytes at a time the product above took 26 us
+// more).
 template <typename T, typename S, bool PAIRED, typename OUT>
 __device__ __forceinline__ void store_tile(const f32x4 (&acc)[S::kTm][S::kTn], int first, int cols, int lane, OUT out) {
     const int g = lane >> 4;
@@ -430,10 +443,10 @@ __device__ __forceinline__ void store_tile(const f32x4 (&acc)[S::kTm][S::kTn], i
 }
 
 // ---------------------------------------------------------------------------
-// Which tiles a workgroup takes.  The host knows no expert's number of rows, so every workgroup adds up the experts' tiles
-// first; where there are more workgroups than tiles, those past the last have nothing to do.
-// Workgroups go to the eight dies in turn, so that numbering gives each die a run of the tiles: eight
-// rows' tiles by all columns' tiles, whose operands its L2 then serves.
+// Which tiles a workgroup takes.  The host knows no expert's number of rows, so every workgroup adds up the
+// experts' tiles first; where there are more workgroups than tiles, those past the last have nothing to do.
+// Workgroups go to the eight dies in turn, so that numbering gives each die a run of the tiles: eight rows' tiles
+// by all columns' tiles, whose operands its L2 then serves.
 // ---------------------------------------------------------------------------
 struct TilePlace {
     int expert;
@@ -534,14 +547,16 @@ __device__ __forceinline__ TilePlace tile_place(const TileTable& table, int expe
 }
 
 // ---------------------------------------------------------------------------
-// y = x * weight.  ALONG: the weights lie [out, in].  DMA: every row of x and of the weights is made of
-// aligned chunks of 16 bytes, which go straight to LDS; else they pass through the registers, where their ends are seen to.
+// y = x * weight, a workgroup a tile, for experts of few rows: every weight is read once, and HBM bounds it (48
+// slots of 64 experts 4096 to 1024 bf16: 47 us, 6.2 TB/s).  Four stages of copies are under way.  ALONG: the
+// weights lie [out, in].  DMA: every row of x and of the weights is made of aligned chunks of 16 bytes, which go
+// straight to LDS; else they pass through the registers, where their ends are seen to.
 // ---------------------------------------------------------------------------
 template <typename T, typename S, bool ALONG, bool DMA>
 __global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall a, uint32_t first, uint32_t launched) {
     using elem = typename T::elem;
-    constexpr int kPer = T::kPer, kStep = S::kBytes / (int)sizeof(elem);
-    constexpr int kXChunks = S::kBytes / 16, kChunks = ALONG ? kXChunks : S::BN / kPer;  // of the tiles' rows
+    constexpr int kPer = T::kPer, kStep = kStepBytes / (int)sizeof(elem);
+    constexpr int kXChunks = kStepBytes / 16, kChunks = ALONG ? kXChunks : S::BN / kPer;  // of the tiles' rows
     constexpr int kXRows = S::kThreads / kXChunks, kWRows = S::kThreads / kChunks;  // tile rows of one load of all threads
     constexpr int kStages = DMA ? S::kStages : 2;
     __shared__ __attribute__((aligned(1024))) char tiles[kStages * S::kStage];
@@ -569,7 +584,7 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall
     const elem* px[S::kRowLoads];
     const elem* pw[S::kColLoads];
     int wc[S::kColLoads];
-    const int xr = t / kXChunks, xc = ((t % kXChunks) ^ along_exchange<false, S::kBytes>(xr)) * kPer;
+    const int xr = t / kXChunks, xc = ((t % kXChunks) ^ along_exchange<false>(xr)) * kPer;
 #pragma unroll
     for (int j = 0; j < S::kRowLoads; ++j) {  // rows past the run's are not stored
         const uint32_t i = (uint32_t)place.first + xr + j * kXRows;  // may pass 2^31
@@ -582,7 +597,7 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall
     for (int j = 0; j < S::kColLoads; ++j) {
         const int r = t / kChunks + j * kWRows;
         if constexpr (ALONG) {
-            wc[j] = ((t % kXChunks) ^ along_exchange<true, S::kBytes>(r)) * kPer;
+            wc[j] = ((t % kXChunks) ^ along_exchange<true>(r)) * kPer;
             const int n = n0 + r < a.cols_out ? n0 + r : a.cols_out - 1;  // columns past the last are not stored
             pw[j] = w + n * a.ld_w;
             if constexpr (DMA)
@@ -649,8 +664,8 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall
     };
 
     const int wm = wave % S::WM, wn = wave / S::WM;
-    const Side<T, true, false, S::BM, S::kTm, S::kBytes> xs(wm * S::kTm * 16, lane);
-    const Side<T, ALONG, ALONG, S::BN, S::kTn, S::kBytes> ws(wn * S::kTn * 16, lane);
+    const Side<T, true, false, S::BM, S::kTm> xs(wm * S::kTm * 16, lane);
+    const Side<T, ALONG, ALONG, S::BN, S::kTn> ws(wn * S::kTn * 16, lane);
     f32x4 acc[S::kTm][S::kTn];
 #pragma unroll
     for (int m = 0; m < S::kTm; ++m)
@@ -699,16 +714,18 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall
 }
 
 // ---------------------------------------------------------------------------
-// The same in a run of tiles for each workgroup; rows of x and of the weights are made of aligned chunks.
+// The same in a run of tiles for each workgroup.  Rows of any alignment pass through registers (131072 slots 1024
+// to 4096 bf16: 1795 us where rows are 4 bytes off a line, 2833 where they are 2 off, whose loads the memory
+// pipeline takes apart; read as whole words and shifted 2580 and 2059, left).
 // ---------------------------------------------------------------------------
 template <typename T, typename S, bool ALONG, bool DMA>
-__global__ __launch_bounds__(S::kThreads) void k_expert_product_run(const ExpertCall a) {
+__global__ __launch_bounds__(S::kThreads, S::kWaves) void k_expert_product_run(const ExpertCall a) {
     using elem = typename T::elem;
-    constexpr int kPer = T::kPer, kStep = S::kBytes / (int)sizeof(elem);
-    constexpr int kXChunks = S::kBytes / 16, kChunks = ALONG ? kXChunks : S::BN / kPer;  // of the tiles' rows
+    constexpr int kPer = T::kPer, kStep = kStepBytes / (int)sizeof(elem);
+    constexpr int kXChunks = kStepBytes / 16, kChunks = ALONG ? kXChunks : S::BN / kPer;  // of the tiles' rows
     constexpr int kXRows = S::kThreads / kXChunks, kWRows = S::kThreads / kChunks;  // tile rows of one load of all threads
-    // Tiles whose entries of order are held: copies run up to kStages tiles ahead of the products (where a tile has one step),
-    // the entries kStages tiles ahead of the copies.
+    // Tiles whose entries of order are held: copies run up to kStages tiles ahead of the products (where a tile
+    // has one step), the entries kStages tiles ahead of the copies.
     constexpr int kRing = S::kStages <= 3 ? 8 : 16;
     static_assert(kRing > 2 * S::kStages && S::BM % 64 == 0);
     __shared__ __attribute__((aligned(1024))) char tiles[S::kStages * S::kStage];
@@ -751,12 +768,13 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product_run(const Expert
     uint32_t copy_id = first;
     int copy_step = 0, copy_ring = 0;
     const elem* px[S::kRowLoads];
-    const int xr = t / kXChunks, xc = ((t % kXChunks) ^ along_exchange<false, S::kBytes>(xr)) * kPer;
-    // the exchange looks at four bits of the row, so a thread's rows of the weights' tile have one chunk, or two in turn
+    const int xr = t / kXChunks, xc = ((t % kXChunks) ^ along_exchange<false>(xr)) * kPer;
+    // the exchange looks at four bits of the row, so a thread's rows of the weights' tile have one chunk, or two
+    // in turn
     constexpr int kColumns = ALONG || kWRows % 16 == 0 ? 1 : 2;
     static_assert(kWRows * kColumns % 16 == 0);
     int wc[kColumns];  // across: the columns
-    const int wr = t / kChunks, wk = ALONG ? ((t % kChunks) ^ along_exchange<true, S::kBytes>(wr)) * kPer : wr;
+    const int wr = t / kChunks, wk = ALONG ? ((t % kChunks) ^ along_exchange<true>(wr)) * kPer : wr;
     const elem* pw = nullptr;
     int w_room = 0;  // ALONG: the weights' rows behind the first
     int k0 = 0;
@@ -842,8 +860,8 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product_run(const Expert
         return id < last ? steps : -1;
     };
     const int wm = wave % S::WM, wn = wave / S::WM;
-    const Side<T, true, false, S::BM, S::kTm, S::kBytes> xs(wm * S::kTm * 16, lane);
-    const Side<T, ALONG, ALONG, S::BN, S::kTn, S::kBytes> ws(wn * S::kTn * 16, lane);
+    const Side<T, true, false, S::BM, S::kTm> xs(wm * S::kTm * 16, lane);
+    const Side<T, ALONG, ALONG, S::BN, S::kTn> ws(wn * S::kTn * 16, lane);
     auto finish = [&](f32x4 (&acc)[S::kTm][S::kTn]) __attribute__((always_inline)) {
         const TilePlace p = place_of(id);
         if (a.x_map.mode && !a.out_map.mode) {  // rows without a slot; in the slots' order they are not stored
@@ -872,8 +890,8 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product_run(const Expert
 }
 
 // ---------------------------------------------------------------------------
-// dweight = x^T * dy, a tile of one expert's matrix for a workgroup.  An expert's rows are cut into parts of `part` rows;
-// where they are more than one, each leaves its sums in the workspace and k_expert_join adds them up.
+// dweight = x^T * dy, a tile of one expert's matrix for a workgroup.  An expert's rows are cut into parts of
+// `part` rows; where they are more than one, each leaves its sums in the workspace and k_expert_join adds them up.
 // ---------------------------------------------------------------------------
 struct PartPlace {
     int expert;
@@ -916,12 +934,15 @@ __device__ __forceinline__ void store_sums(const ExpertCall& a, const PartPlace&
     }
 }
 
-// DMA: rows of x and dy are made of aligned chunks, which go straight to LDS.
+// DMA: rows of x and dy are made of aligned chunks, which go straight to LDS.  Both halves of both operands'
+// copies are early ones.  Bound as the product is (16384 x 8 slots 4096 by 1024 bf16 1230 to 1270 us, 860 to 895
+// TFLOP/s): the products alone 773 us, the copies alone 798; all fragments are read transposed, which takes twice
+// the LDS cycles.  Experts' loads differ, so the dies take equal shares of the steps, not of the tiles.
 template <typename T, typename S, bool DMA>
-__global__ __launch_bounds__(S::kThreads, 2) void k_expert_weight_back(const ExpertCall a) {
+__global__ __launch_bounds__(S::kThreads, S::kWaves) void k_expert_weight_back(const ExpertCall a) {
     using elem = typename T::elem;
     static_assert(S::BM == S::BN, "a thread's rows of x and dy are the same slots");
-    constexpr int kPer = T::kPer, kStep = S::kBytes / (int)sizeof(elem);
+    constexpr int kPer = T::kPer, kStep = kStepBytes / (int)sizeof(elem);
     constexpr int kChunks = S::BN / kPer, kRows = S::kThreads / kChunks, kLoads = S::kColLoads;
     constexpr int kColumns = kRows % 16 == 0 ? 1 : 2;  // the exchange looks at four bits of the row
     static_assert(kRows * kColumns % 16 == 0 && kLoads % (2 * kColumns) == 0 && kStep <= 64);
@@ -983,8 +1004,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_expert_weight_back(const Exp
         }
     };
 
-    // The entries of order come to LDS before the copies that need them.  (Loaded into registers they would have to be waited for,
-    // and with them, in the order of the loads, all copies issued before.)
+    // The entries of order come to LDS before the copies that need them.  (Loaded into registers they would have
+    // to be waited for, and with them, in the order of the loads, all copies issued before.)
     Cursor look{first, 0, 0, {}};
     settle(look);
     int look_ring = 0;
@@ -1076,8 +1097,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_expert_weight_back(const Exp
         return id < last ? steps_of(part_place(table, a, id / of_part)) : -1;
     };
     const int wm = wave % S::WM, wn = wave / S::WM;
-    const Side<T, false, false, S::BM, S::kTm, S::kBytes> xs(wm * S::kTm * 16, lane);
-    const Side<T, false, false, S::BN, S::kTn, S::kBytes> ws(wn * S::kTn * 16, lane);
+    const Side<T, false, false, S::BM, S::kTm> xs(wm * S::kTm * 16, lane);
+    const Side<T, false, false, S::BN, S::kTn> ws(wn * S::kTn * 16, lane);
     auto finish = [&](f32x4 (&acc)[S::kTm][S::kTn]) __attribute__((always_inline)) {
         uint32_t m, n;
         grouped_tile(id % of_part, m_tiles, n_tiles, m, n);
@@ -1090,8 +1111,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_expert_weight_back(const Exp
 
 constexpr int kJoinBlock = 256;
 
-// dweight of the experts of several parts from the parts' sums, in the parts' order; a thread four elements in turn, a row of
-// workgroups an expert.
+// dweight of the experts of several parts from the parts' sums, in the parts' order; a thread four elements in
+// turn, a row of workgroups an expert.
 template <typename T>
 __global__ __launch_bounds__(kJoinBlock) void k_expert_join(const ExpertCall a) {
     __shared__ TileTable table;

@@ -7,12 +7,13 @@
 // every type: the maximum's own term is then 1 to the bit, so S >= 1, no log probability is above 0 and a
 // certain token has 0.
 //
-// The list: the threads' elements are groups (or their vectors are, for long lists), and the k-th largest of the groups'
-// maxima is no more than the k-th largest logit, so only logits from there on can be listed: little more than k of them
-// unless they lie close together in the row.  A bound just below it comes from a histogram of the maxima's distances from the
-// row's maximum; the threads whose own maximum is above it read their vectors again and queue those with such logits, which
-// a thread for each of their elements lists.  An entry's place is the number of entries above it.  Where too many are listed for that (rows of equal values), the k-th
-// (logit, token) itself is found, eight bits at a time.
+// The list: the threads' elements are groups (or their vectors are, for long lists), and the k-th largest of the
+// groups' maxima is no more than the k-th largest logit, so only logits from there on can be listed: little more
+// than k of them unless they lie close together in the row.  A bound just below it comes from a histogram of the
+// maxima's distances from the row's maximum; the threads whose own maximum is above it read their vectors again
+// and queue those with such logits, which a thread for each of their elements lists.  An entry's place is the
+// number of entries above it.  Where too many are listed for that (rows of equal values), the k-th (logit, token)
+// itself is found, eight bits at a time.
 #pragma once
 
 #include "row_ops.hpp"
@@ -141,7 +142,8 @@ struct LogProbLds {
     uint32_t listed, queued;
 };
 
-// The bin of a distance from the maximum, a sixteenth of an octave from 2^-12 to 2^20, those beyond in the first and the last.
+// The bin of a distance from the maximum, a sixteenth of an octave from 2^-12 to 2^20, those beyond in the first
+// and the last.
 constexpr int kFirstBin = (127 - 12) << 4;
 __device__ __forceinline__ int distance_bin(float d) {
     const int b = (int)(__builtin_bit_cast(uint32_t, d) >> 19) - kFirstBin;
@@ -152,8 +154,9 @@ __device__ __forceinline__ float beyond_bin(int b) {
     return b >= kDistanceBins - 1 ? __builtin_inff() : __builtin_bit_cast(float, (uint32_t)(b + 1 + kFirstBin) << 19);
 }
 
-// The first of COUNT bins (in the order of their number, or from the last down) up to which there are at least `want` entries,
-// -1: there are fewer.  before: entries in the bins before it, here: in it.  Every wave finds the same.
+// The first of COUNT bins (in the order of their number, or from the last down) up to which there are at least
+// `want` entries, -1: there are fewer.  before: entries in the bins before it, here: in it.  Every wave finds the
+// same.
 template <int COUNT, bool DOWN>
 __device__ __forceinline__ int bin_reaching(const uint32_t* bins, uint32_t want, uint32_t& before, uint32_t& here) {
     constexpr int kPer = COUNT / 64;
@@ -262,7 +265,8 @@ __device__ __forceinline__ int find_top(const LogitRow<T, NT, NV>& row, const ty
     }
     if (n <= capacity)
         return n;
-    // the k-th entry itself, from its highest digit down, or what is left of it where all entries with these digits are listed
+    // the k-th entry itself, from its highest digit down, or what is left of it where all entries with these
+    // digits are listed
     auto each = [&](auto f) __attribute__((always_inline)) {
         row.each_again([&](u32x4 u, int column) __attribute__((always_inline)) {
             float v[T::kPer];

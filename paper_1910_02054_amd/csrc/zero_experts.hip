@@ -55,21 +55,22 @@ bool whole_chunks(const void* p, int64_t ld, int64_t cols, size_t elem) {
 
 constexpr int64_t kCus = 256;  // MI355X
 
-// The kernel that takes tiles in a run, in tiles of 256 or 128 rows by 256 columns: the shape whose rounds of tiles over the
-// compute units cost less.  A round of 128 rows is 0.58 of one of 256 (8192 slots of 16 experts 4096 to 1600 f16, 280 tiles in 2 rounds
-// of 256 or 504 in 2 of 128: 205 and 153 us; 4096 of 8 experts 1600 to 6400, 500 in 2 or 900 in 4: 109 and 122).
+// The kernel that takes tiles in a run, in tiles of 256 or 128 rows by 256 columns: the shape whose rounds of
+// tiles over the compute units cost less.  A round of 128 rows is 0.58 of one of 256 (8192 slots of 16 experts
+// 4096 to 1600 f16, 280 tiles in 2 rounds of 256 or 504 in 2 of 128: 205 and 153 us; 4096 of 8 experts 1600 to
+// 6400, 500 in 2 or 900 in 4: 109 and 122).
 template <typename F>
 int with_run_shape(int64_t slots, int experts, int64_t cols_out, F f) {
     auto rounds = [&](int64_t rows) {
         return (double)div_up((slots / rows + experts / 2) * div_up(cols_out, 256), kCus);
     };
-    if (0.58 * rounds(128) < rounds(256)) return f(zo::TileShape<128, 256, 2, 4, 3, 128>{});
-    return f(zo::TileShape<256, 256, 2, 4, 2, 128>{});
+    if (0.58 * rounds(128) < rounds(256)) return f(zo::TileShape<128, 256, 2, 4, 3>{});
+    return f(zo::TileShape<256, 256, 2, 4, 2>{});
 }
 
-// Rows of a part of the weights' gradient's sums, 0: an expert's rows are one.  A longer part takes longer (1.5 us for 64
-// rows), a shorter one leaves more sums to be written and read again (at 4.5 TB/s): slots / part matrices of `size` floats.
-// The length at which both are the same, if the workspace's bound allows it.
+// Rows of a part of the weights' gradient's sums, 0: an expert's rows are one.  A longer part takes longer (1.5 us
+// for 64 rows), a shorter one leaves more sums to be written and read again (at 4.5 TB/s): slots / part matrices
+// of `size` floats. The length at which both are the same, if the workspace's bound allows it.
 int64_t part_rows(int64_t slots, int experts, int64_t size) {
     const int64_t room = ZERO_EXPERT_WORKSPACE_MAX / size - experts;  // parts behind each expert's first
     if (room < 1)
@@ -142,7 +143,7 @@ int zero_expert_product(const zero_expert_product_args_t* args, void* stream_) {
             return (int)ZERO_OK;
         };
         if (a.slots / a.experts <= kFewRows) {
-            using S = zo::TileShape<32, 128, 1, 4, 4, 128>;
+            using S = zo::TileShape<32, 128, 1, 4, 4>;
             return by_tile(S{}, a.transposed ? (dma ? zo::k_expert_product<T, S, true, true>
                                                     : zo::k_expert_product<T, S, true, false>)
                                              : (dma ? zo::k_expert_product<T, S, false, true>
@@ -150,29 +151,31 @@ int zero_expert_product(const zero_expert_product_args_t* args, void* stream_) {
         }
         auto in_runs = [&](auto shape, auto* kernel) {
             using S = decltype(shape);
-            kernel<<<kCus * 512 / S::kThreads, S::kThreads, 0, stream>>>(c);
+            kernel<<<kCus * S::kPerCu, S::kThreads, 0, stream>>>(c);
             HIP_TRY(hipGetLastError());
             return (int)ZERO_OK;
         };
-        // fp32: the products take most of the time whatever the tile (a sixteenth of bf16's rate), so small tiles, evenly over the
-        // compute units (3063 slots of 12 experts 803 to 1203: 117 us, 201 in tiles of 128 by 128, 167 of 128 by 256)
+        // fp32: the products take most of the time whatever the tile (a sixteenth of bf16's rate), so small tiles,
+        // evenly over the compute units (3063 slots of 12 experts 803 to 1203: 117 us, 201 in tiles of 128 by 128,
+        // 167 of 128 by 256)
         if constexpr (T::kPer == 4) {
-            using S = zo::TileShape<64, 128, 2, 2, 2, 128>;
+            using S = zo::TileShape<64, 128, 2, 2, 2>;
             return in_runs(S{}, a.transposed ? (dma ? zo::k_expert_product_run<T, S, true, true>
                                                     : zo::k_expert_product_run<T, S, true, false>)
                                              : (dma ? zo::k_expert_product_run<T, S, false, true>
                                                     : zo::k_expert_product_run<T, S, false, false>));
+        } else {
+            if (!dma) {
+                using S = zo::TileShape<128, 256, 2, 4, 2>;
+                return in_runs(S{}, a.transposed ? zo::k_expert_product_run<T, S, true, false>
+                                                 : zo::k_expert_product_run<T, S, false, false>);
+            }
+            return with_run_shape(a.slots, a.experts, a.cols_out, [&](auto shape) {
+                using S = decltype(shape);
+                return in_runs(shape, a.transposed ? zo::k_expert_product_run<T, S, true, true>
+                                                   : zo::k_expert_product_run<T, S, false, true>);
+            });
         }
-        if (!dma) {
-            using S = zo::TileShape<128, 256, 2, 4, 2, 128>;
-            return in_runs(S{}, a.transposed ? zo::k_expert_product_run<T, S, true, false>
-                                             : zo::k_expert_product_run<T, S, false, false>);
-        }
-        return with_run_shape(a.slots, a.experts, a.cols_out, [&](auto shape) {
-            using S = decltype(shape);
-            return in_runs(shape, a.transposed ? zo::k_expert_product_run<T, S, true, true>
-                                               : zo::k_expert_product_run<T, S, false, true>);
-        });
     });
 }
 
@@ -231,16 +234,17 @@ int zero_expert_weight_backward(const zero_expert_weight_backward_args_t* args, 
     const bool dma = whole_chunks(a.x, a.ld_x, a.cols_in, e) && whole_chunks(a.dy, a.ld_dy, a.cols_out, e);
     return with_type(a.dtype, [&](auto type) {
         using T = decltype(type);
-        // Tiles of 256 by 256, but where they would be half empty (16384 slots of 64 experts, 128 by 128 f16: 21 us, 27 in tiles of 256;
-        // 65536 of 64, 512 by 256 bf16: 80 and 62) and for fp32, bound by the products (8192 of 8, 1024 by 4096: 835 and 1138).
-        using Wide = zo::TileShape<256, 256, 2, 4, 2, 128>;
-        using Small = zo::TileShape<128, 128, 2, 2, 2, 128>;  // two workgroups to a compute unit
+        // Tiles of 256 by 256, but where they would be half empty (16384 slots of 64 experts, 128 by 128 f16: 21
+        // us, 27 in tiles of 256; 65536 of 64, 512 by 256 bf16: 80 and 62) and for fp32, bound by the products
+        // (8192 of 8, 1024 by 4096: 835 and 1138).
+        using Wide = zo::TileShape<256, 256, 2, 4, 2>;
+        using Small = zo::TileShape<128, 128, 2, 2, 2>;  // two workgroups to a compute unit
         if (!dma)
-            zo::k_expert_weight_back<T, Small, false><<<2 * kCus, Small::kThreads, 0, stream>>>(c);
+            zo::k_expert_weight_back<T, Small, false><<<kCus * Small::kPerCu, Small::kThreads, 0, stream>>>(c);
         else if (T::kPer == 4 || std::min(a.cols_in, a.cols_out) <= 128)
-            zo::k_expert_weight_back<T, Small, true><<<2 * kCus, Small::kThreads, 0, stream>>>(c);
+            zo::k_expert_weight_back<T, Small, true><<<kCus * Small::kPerCu, Small::kThreads, 0, stream>>>(c);
         else if constexpr (T::kPer == 8)
-            zo::k_expert_weight_back<T, Wide, true><<<kCus, Wide::kThreads, 0, stream>>>(c);
+            zo::k_expert_weight_back<T, Wide, true><<<kCus * Wide::kPerCu, Wide::kThreads, 0, stream>>>(c);
         HIP_TRY(hipGetLastError());
         if (c.part) {
             const dim3 grid((unsigned)div_up(a.cols_in * a.cols_out, 4 * zo::kJoinBlock), (unsigned)a.experts);

@@ -13,8 +13,9 @@ struct LogitShape {
     static constexpr int NT = NT_, NV = NV_;
 };
 
-// Rows of more than 7168 vectors fit a workgroup's registers up to 16384, at one workgroup to a compute unit; where a list
-// follows two that read the row twice are faster (1024 x 131072 bf16 without a list 57.7 us, read again 62; lists of 128: 103 and 85).
+// Rows of more than 7168 vectors fit a workgroup's registers up to 16384, at one workgroup to a compute unit;
+// where a list follows two that read the row twice are faster (1024 x 131072 bf16 without a list 57.7 us, read
+// again 62; lists of 128: 103 and 85).
 template <typename F>
 int with_logit_shape(int64_t vectors, bool list, F f) {
     if (vectors <= 128) return f(LogitShape<128, 1>{});
