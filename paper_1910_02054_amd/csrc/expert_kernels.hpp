@@ -167,7 +167,7 @@ struct TileShape {
     static constexpr int kRowsBytes = BM * kStepBytes, kColsBytes = BN * kStepBytes, kStage = kRowsBytes + kColsBytes;
     static constexpr int kRowLoads = kRowsBytes / 16 / kThreads, kColLoads = kColsBytes / 16 / kThreads;  // a thread's
     static constexpr int kCopies = kRowLoads + kColLoads;
-    static constexpr int kPerCu = kStages * kStage > 80 * 1024 ? 1 : 2;  // workgroups, by their LDS
+    static constexpr int kPerCu = 160 * 1024 / (kStages * kStage + 14 * 1024);  // workgroups, by their LDS
     static constexpr int kWaves = kPerCu * WM * WN / 4;                  // of a SIMD
     static_assert(kRowLoads * 16 * kThreads == kRowsBytes && kColLoads * 16 * kThreads == kColsBytes, "whole loads");
 };

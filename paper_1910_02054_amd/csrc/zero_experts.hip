@@ -156,10 +156,10 @@ int zero_expert_product(const zero_expert_product_args_t* args, void* stream_) {
             return (int)ZERO_OK;
         };
         // fp32: the products take most of the time whatever the tile (a sixteenth of bf16's rate), so small tiles,
-        // evenly over the compute units (3063 slots of 12 experts 803 to 1203: 117 us, 201 in tiles of 128 by 128,
-        // 167 of 128 by 256)
+        // evenly over the compute units, three workgroups to each (3063 slots of 12 experts 803 to 1203: 102 us, 116
+        // in tiles of 64 by 128, 201 of 128 by 128; 1065 of 8 experts 6943 to 3769: 997 and 1401 of 64 by 128)
         if constexpr (T::kPer == 4) {
-            using S = zo::TileShape<64, 128, 2, 2, 2>;
+            using S = zo::TileShape<64, 64, 2, 2, 2>;
             return in_runs(S{}, a.transposed ? (dma ? zo::k_expert_product_run<T, S, true, true>
                                                     : zo::k_expert_product_run<T, S, true, false>)
                                              : (dma ? zo::k_expert_product_run<T, S, false, true>

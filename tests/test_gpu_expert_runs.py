@@ -17,7 +17,7 @@ pytestmark = pytest.mark.gpu
 F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
 
 
-# 256 compute units take tiles of 256 or 128 rows by 256 columns (fp32: 64 by 128): three to six tiles for each workgroup, of
+# 256 compute units take tiles of 256 or 128 rows by 256 columns (fp32: 64 by 64): several tiles for each workgroup, of
 # one step, of two, the last of them short, and of seven
 @pytest.mark.parametrize("dtype", C.TYPES)
 @pytest.mark.parametrize("transposed", (False, True))
