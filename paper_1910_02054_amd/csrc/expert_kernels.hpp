@@ -221,7 +221,8 @@ __device__ __forceinline__ void wait_stage() {
 
 // The tiles that a workgroup takes, one after another, as one run of steps: the copies of a tile's first steps are
 // under way before the tile before it has ended, and its results are stored while they land.
-//   next_step()          prepares the copies of the run's next step; false: there is none
+//   next_step()          prepares the copies of the run's next step; false: there is none.  What one call asks of
+//                        LDS for a step kStages later is there: all waves have met since
 //   copy(i, stage)       issues copy i of that step, into the stage at LDS address `stage`
 //   tile_steps()         the steps of the next tile, below 0: none
 //   finish(acc)          stores a tile's results
@@ -260,17 +261,17 @@ __device__ __forceinline__ void multiply_tiles(char* tiles, uint32_t lds, const 
         if (!DMA && more)
             put(tiles + s * S::kStage);
     }
+    if (DMA && more)
+        wait_stage<(S::kStages - 1) * S::kCopies + EARLY>();
+    else
+        wait_stage<0>();
     if constexpr (!DMA) {
-        more = more && next_step();
+        more = more && next_step();  // behind the wait: it may need what all waves brought in the first step
         if (more)
 #pragma unroll
             for (int i = 0; i < S::kCopies; ++i)
                 copy(i, 0);
     }
-    if (DMA && more)
-        wait_stage<(S::kStages - 1) * S::kCopies + EARLY>();
-    else
-        wait_stage<0>();
     u32x4 xf[S::kTm], wf[S::kTn], wn[S::kTn];
 #pragma unroll
     for (int n = 0; n < S::kTn; ++n)
@@ -726,9 +727,9 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void k_expert_product_run(c
     constexpr int kXChunks = kStepBytes / 16, kChunks = ALONG ? kXChunks : S::BN / kPer;  // of the tiles' rows
     constexpr int kXRows = S::kThreads / kXChunks, kWRows = S::kThreads / kChunks;  // tile rows of one load of all threads
     // Tiles whose entries of order are held: copies run up to kStages tiles ahead of the products (where a tile
-    // has one step), the entries kStages tiles ahead of the copies.
+    // has one step; through registers one tile more), the entries kStages tiles ahead of the copies.
     constexpr int kRing = S::kStages <= 3 ? 8 : 16;
-    static_assert(kRing > 2 * S::kStages && S::BM % 64 == 0);
+    static_assert(kRing > 2 * S::kStages + (DMA ? 0 : 1) && S::BM % 64 == 0);
     __shared__ __attribute__((aligned(1024))) char tiles[S::kStages * S::kStage];
     __shared__ int32_t slots_of[kRing][S::BM];
     __shared__ TileTable table;
