@@ -195,16 +195,20 @@ __device__ __forceinline__ void multiply(const char* stage, const XS& xs, const 
 // 16 bytes straight to LDS: lane l's land at base + 16 l.  Written as an instruction because the compiler holds
 // every ds_read_tr behind all copies that it knows of (s_waitcnt vmcnt(0) before the step's first fragment: of the
 // simplest kernel 16384 x 8 slots 1024 to 4096 bf16 took 1612 us, 1300 with this); wait_stage has the waits.
-// There is
-// no output register, and nothing else in these kernels uses m0.
+// There is no output register.  m0 is named as overwritten: the compiler sets it once for several instructions of its
+// own that want the same value, and would not set it again behind this one.  (It warns that it does not keep a
+// reserved register's value across the statement, which is what is wanted.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void copy_to_lds(const void* from, uint32_t base) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(base), "v"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(base), "v"(from) : "m0", "memory");
 }
 
 // 4 bytes, lane l's to base + 4 l.
 __device__ __forceinline__ void copy_word_to_lds(const void* from, uint32_t base) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(base), "v"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(base), "v"(from) : "m0", "memory");
 }
+#pragma clang diagnostic pop
 
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)ZO_LDS(const void, p); }
 
