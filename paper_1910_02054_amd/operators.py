@@ -359,14 +359,23 @@ def zero_expert_weight_backward(x, dy, offsets, dweight, workspace=None, order=N
         _check(rc)
 
 
+def _slots_of_token(index, y, tokens):
+    """k, from index [tokens, k] or, where that is None, from y [tokens * k, cols]."""
+    if index is not None:
+        return index.shape[-1]
+    if y is None:
+        raise ValueError("without index, y or dy must be given")
+    return _sizes(y, "y")[0] // tokens if tokens else 1
+
+
 def zero_expert_mix(y, index, out, weight=None, base=None, experts=0, stream=None):
     """out[t] = base[t] + sum over i of weight[t][i] * y[t * k + i], over the slots with an expert: index (int32,
-    [tokens, k]) not below 0 and, where experts is not 0, below it.  y [tokens * k, cols]; weight float32 [tokens, k]
-    (None: 1); base like out (None: 0), which may be base in place."""
+    [tokens, k]; None: every slot has one) not below 0 and, where experts is not 0, below it.  y [tokens * k, cols];
+    weight float32 [tokens, k] (None: 1); base like out (None: 0), which may be base in place."""
     code, dt = _type(out, "out"), out.dtype
     dev = out.get_device()
     size = tokens, cols = _sizes(out, "out")
-    k = index.shape[-1]
+    k = _slots_of_token(index, y, tokens)
     po, ld_o = _matrix(out, dt, "out", size, dev)
     py, ld_y = _matrix(y, dt, "y", (tokens * k, cols), dev)
     pb, ld_b = _matrix(base, dt, "base", size, dev)
@@ -380,11 +389,11 @@ def zero_expert_mix(y, index, out, weight=None, base=None, experts=0, stream=Non
 def zero_expert_mix_backward(dout, y, index, weight, dy, dweight=None, experts=0, stream=None):
     """The gradients of zero_expert_mix from dout [tokens, cols]: dy [tokens * k, cols] (may be y in place; None: not
     wanted) and dweight [tokens, k] float32 (None: not wanted, then y is None too); both 0 in slots without an
-    expert.  base's gradient is dout."""
+    expert (index None: every slot has one).  base's gradient is dout."""
     code, dt = _type(dout, "dout"), dout.dtype
     dev = dout.get_device()
     size = tokens, cols = _sizes(dout, "dout")
-    k = index.shape[-1]
+    k = _slots_of_token(index, dy if y is None else y, tokens)
     pd, ld_d = _matrix(dout, dt, "dout", size, dev)
     py, ld_y = _matrix(y, dt, "y", (tokens * k, cols), dev)
     pdy, ld_dy = _matrix(dy, dt, "dy", (tokens * k, cols), dev)

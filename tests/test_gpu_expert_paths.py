@@ -157,3 +157,32 @@ def test_entries_of_order_that_name_no_slot(zo, tokens, cin, cout, lead, dtype):
         torch.cuda.synchronize()
         assert out.guards_intact() and room.guards_intact()
         C.within(out.view.unflatten(0, (experts, cin)), want, C.rounded(bound, want, dtype), "dw")
+
+
+@pytest.mark.parametrize("dtype", C.TYPES)
+@pytest.mark.parametrize("tokens,k,cols", ((1, 1, 5), (7, 3, 264), (40, 8, 130)))
+def test_mix_where_every_slot_has_an_expert(zo, tokens, k, cols, dtype):  # noqa: F811
+    """Without an index k is that of y's rows, and nothing is left out."""
+    g = C.rng(43, tokens, k, cols)
+    y, dout, w = C.normal(g, tokens * k, cols).to(dtype), C.normal(g, tokens, cols).to(dtype), C.normal(g, tokens, k).float()
+    every = torch.zeros(tokens, k, dtype=torch.int32)
+    dy, dw, db = E.mix_backward(dout, y, every, w)
+    yd, dd = y.cuda(), dout.cuda()
+    for weight in (None, w):
+        want, bound = E.mix(y, every, weight, None)
+        out = torch.empty_like(dd)
+        zo.zero_expert_mix(yd, None, out, weight=None if weight is None else weight.cuda())
+        C.within(out, want, C.rounded(bound, want, dtype), "out")
+    got, gw = torch.empty_like(yd), torch.empty(tokens, k, device="cuda")
+    zo.zero_expert_mix_backward(dd, yd, None, w.cuda(), got, gw)
+    C.within(got, dy, C.rounded(C.U * dy.abs(), dy, dtype), "dy")
+    C.within(gw, dw, db, "dweight")
+    alone = torch.empty_like(yd)
+    zo.zero_expert_mix_backward(dd, None, None, w.cuda(), alone)
+    assert torch.equal(alone, got)
+    none = torch.empty(0, cols, dtype=dtype, device="cuda")
+    zo.zero_expert_mix(none, None, none.clone())
+    with pytest.raises(ValueError):
+        zo.zero_expert_mix(yd, None, torch.empty(tokens + 1, cols, dtype=dtype, device="cuda"))
+    with pytest.raises(ValueError):
+        zo.zero_expert_mix_backward(dd, None, None, w.cuda(), None)
