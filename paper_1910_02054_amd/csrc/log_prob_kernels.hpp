@@ -52,6 +52,35 @@ __device__ __forceinline__ void move_sums(const Exponent& to, float from, float&
     s = s == 0.f ? 0.f : f * s;
 }
 
+// A thread's sums of a long row, in 64 bits: s and u hold those of the latest kVectors vectors, so that a row of any
+// length has no more than 512 roundings to 32 bits in turn (without, a row of 2^26 logits of two values 1 apart, 2^16
+// terms a thread, had a sum that was off by 3e-4).
+struct LongSums {
+    static constexpr int kVectors = 64;
+    double s = 0.0, u = 0.0;
+    int held = 0;
+    // As move_sums.
+    __device__ __forceinline__ void move(const Exponent& to, float from) {
+        if (s == 0.0)
+            return;
+        const float d = bounded(to(Exponent(to.c, from).m)), f = exp2_fast(d);
+        u = (double)f * ((double)d * s + u);
+        s = (double)f * s;
+    }
+    __device__ __forceinline__ void fold(float& s32, float& u32) {
+        if (++held == kVectors) {
+            s += (double)s32;
+            u += (double)u32;
+            s32 = u32 = 0.f;
+            held = 0;
+        }
+    }
+    __device__ __forceinline__ void join(float& s32, float& u32) const {
+        s32 = (float)(s + (double)s32);
+        u32 = (float)(u + (double)u32);
+    }
+};
+
 // (a - b) / temperature without leaving fp32 on the way.
 __device__ __forceinline__ float scaled_difference(float a, float b, float inverse) {
     return 2.f * ((0.5f * a - 0.5f * b) * inverse);
@@ -353,10 +382,12 @@ __global__ __launch_bounds__(NT) void k_log_probs(const zero_log_probs_args_t a,
     } else {
         m = row.edge == row.edge ? row.edge : -inf;
         add_term(row.edge, Exponent(k.c, m), s, u);
+        LongSums sums;
         row.each([&](u32x4 v, int) __attribute__((always_inline)) {
             const float up = max_of<T>(v, m);
             const Exponent x(k.c, up);
             if (up > m) {
+                sums.move(x, m);
                 move_sums(x, m, s, u);
                 m = up;
             }
@@ -365,7 +396,9 @@ __global__ __launch_bounds__(NT) void k_log_probs(const zero_log_probs_args_t a,
 #pragma unroll
             for (int j = 0; j < T::kPer; ++j)
                 add_term(f[j], x, s, u);
+            sums.fold(s, u);
         });
+        sums.join(s, u);
         most = m;
         m = seg_reduce<64>(most, Max());
         move_sums(Exponent(k.c, m), most, s, u);
