@@ -172,6 +172,46 @@ struct TileShape {
     static_assert(kRowLoads * 16 * kThreads == kRowsBytes && kColLoads * 16 * kThreads == kColsBytes, "whole loads");
 };
 
+// The product's long sums in fp32: what kFoldSteps steps have added up goes into sums of its own, so that no chain of
+// roundings is longer than 512 products and one for each 512 behind them (in one chain 8193 products of 0.9 were
+// off by 7e-5 of their sum, 262144 by 2e-3).  The 16-bit types add 32 products at a time: up to 131072 of them their roundings of 2^-24 stay
+// below the result's own, 2^-12 or 2^-9.
+constexpr int kFoldSteps = 16;
+
+template <bool USED, typename S>
+struct Folded {
+    f32x4 sum[USED ? S::kTm : 1][USED ? S::kTn : 1];
+    __device__ __forceinline__ Folded() {
+        if constexpr (USED)
+#pragma unroll
+            for (int m = 0; m < S::kTm; ++m)
+#pragma unroll
+                for (int n = 0; n < S::kTn; ++n)
+                    sum[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // Behind step s of a tile.
+    __device__ __forceinline__ void fold(int s, f32x4 (&acc)[S::kTm][S::kTn]) {
+        if constexpr (USED)
+            if (s % kFoldSteps == kFoldSteps - 1) {
+#pragma unroll
+                for (int m = 0; m < S::kTm; ++m)
+#pragma unroll
+                    for (int n = 0; n < S::kTn; ++n) {
+                        sum[m][n] += acc[m][n];
+                        acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    }
+            }
+    }
+    __device__ __forceinline__ void join(f32x4 (&acc)[S::kTm][S::kTn]) const {
+        if constexpr (USED)
+#pragma unroll
+            for (int m = 0; m < S::kTm; ++m)
+#pragma unroll
+                for (int n = 0; n < S::kTn; ++n)
+                    acc[m][n] += sum[m][n];
+    }
+};
+
 // The step's part of a wave's results.
 template <typename T, typename S, typename XS, typename WS>
 __device__ __forceinline__ void multiply(const char* stage, const XS& xs, const WS& ws, f32x4 (&acc)[S::kTm][S::kTn]) {
@@ -245,8 +285,8 @@ __device__ __forceinline__ void wait_stage() {
 // 1186; the early halves 1146.  Tried and left: steps of 64 bytes in four stages (half lines copied: 1315), lines
 // touched ahead for L2 (1229), four waves of 128 by 128 (2830: one wave a SIMD), stores past the caches, a raised
 // wave priority and groups of 4 or 16 row tiles (no difference).
-template <typename T, typename S, bool DMA, int EARLY, typename XS, typename WS, typename NEXT, typename COPY, typename PUT,
-          typename STEPS, typename FINISH>
+template <typename T, typename S, bool DMA, bool FOLD, int EARLY, typename XS, typename WS, typename NEXT, typename COPY,
+          typename PUT, typename STEPS, typename FINISH>
 __device__ __forceinline__ void multiply_tiles(char* tiles, uint32_t lds, const XS& xs, const WS& ws, NEXT next_step,
                                                COPY copy, PUT put, STEPS tile_steps, FINISH finish) {
     constexpr int kLead = S::kTm / 2, kGroups = 2 * S::kTm;
@@ -291,6 +331,7 @@ __device__ __forceinline__ void multiply_tiles(char* tiles, uint32_t lds, const 
 #pragma unroll
             for (int n = 0; n < S::kTn; ++n)
                 acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+        Folded<FOLD, S> folded;
         for (int s = 0; s < steps; ++s) {
             const char* from = tiles + at * S::kStage;
             const uint32_t stage = lds + at * S::kStage;
@@ -345,7 +386,9 @@ __device__ __forceinline__ void multiply_tiles(char* tiles, uint32_t lds, const 
                     for (int n = 0; n < S::kTn; ++n)
                         wf[n] = wn[n];
             }
+            folded.fold(s, acc);
         }
+        folded.join(acc);
         finish(acc);
     }
 }
@@ -558,8 +601,10 @@ __device__ __forceinline__ TilePlace tile_place(const TileTable& table, int expe
 // weights lie [out, in].  DMA: every row of x and of the weights is made of aligned chunks of 16 bytes, which go
 // straight to LDS; else they pass through the registers, where their ends are seen to.
 // ---------------------------------------------------------------------------
+// (Two waves a SIMD are asked for in fp32 so that the sums stay in registers that additions take too: kept in the
+// accumulation registers they went back and forth every step, 64 slots of 8 experts 4096 to 1024: 95 us and 87.)
 template <typename T, typename S, bool ALONG, bool DMA>
-__global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall a, uint32_t first, uint32_t launched) {
+__global__ __launch_bounds__(S::kThreads, T::kPer == 4 ? 2 : 1) void k_expert_product(const ExpertCall a, uint32_t first, uint32_t launched) {
     using elem = typename T::elem;
     constexpr int kPer = T::kPer, kStep = kStepBytes / (int)sizeof(elem);
     constexpr int kXChunks = kStepBytes / 16, kChunks = ALONG ? kXChunks : S::BN / kPer;  // of the tiles' rows
@@ -679,6 +724,7 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall
         for (int n = 0; n < S::kTn; ++n)
             acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
 
+    Folded<T::kPer == 4, S> folded;
     constexpr int kAhead = kStages - 1;  // stages under way
 #pragma unroll
     for (int s = 0; s < kAhead; ++s)
@@ -695,9 +741,11 @@ __global__ __launch_bounds__(S::kThreads) void k_expert_product(const ExpertCall
         if (s + kAhead < steps)
             fetch(s + kAhead);
         multiply<T, S>(tiles + s % kStages * S::kStage, xs, ws, acc);
+        folded.fold(s, acc);
         if (s + kAhead < steps)
             put(s + kAhead);
     }
+    folded.join(acc);
 
     if (a.x_map.mode && !a.out_map.mode) {  // rows without a slot; in the slots' order they are not stored
 #pragma unroll
@@ -892,7 +940,8 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void k_expert_product_run(c
             look_up(first + i * stride, i);
         wait_stage<0>();
     }
-    multiply_tiles<T, S, DMA, kEarly>(tiles, lds_address(tiles) + wave * 1024, xs, ws, next_step, copy, put, tile_steps, finish);
+    multiply_tiles<T, S, DMA, T::kPer == 4, kEarly>(tiles, lds_address(tiles) + wave * 1024, xs, ws, next_step, copy, put,
+                                                    tile_steps, finish);
 }
 
 // ---------------------------------------------------------------------------
@@ -1111,8 +1160,8 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void k_expert_weight_back(c
         store_sums<T, S>(a, part_place(table, a, id / of_part), acc, (int)m * S::BM + wm * S::kTm * 16,
                          (int)n * S::BN + wn * S::kTn * 16, lane);
     };
-    multiply_tiles<T, S, DMA, DMA ? 2 * kHalf : 0>(tiles, lds_address(tiles) + wave * 1024, xs, ws, next_step, copy, put,
-                                                   tile_steps, finish);
+    multiply_tiles<T, S, DMA, false, DMA ? 2 * kHalf : 0>(tiles, lds_address(tiles) + wave * 1024, xs, ws, next_step, copy,
+                                                          put, tile_steps, finish);
 }
 
 constexpr int kJoinBlock = 256;

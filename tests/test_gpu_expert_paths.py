@@ -186,3 +186,23 @@ def test_mix_where_every_slot_has_an_expert(zo, tokens, k, cols, dtype):  # noqa
         zo.zero_expert_mix(yd, None, torch.empty(tokens + 1, cols, dtype=dtype, device="cuda"))
     with pytest.raises(ValueError):
         zo.zero_expert_mix_backward(dd, None, None, w.cuda(), None)
+
+
+@pytest.mark.parametrize("lead", (0, LEAD))
+@pytest.mark.parametrize("rows,cin,cout", ((20, 262144, 8), (60, 262144, 8), (20, 8193, 40), (60, 5000, 72), (130, 65536, 16)))
+def test_long_sums_in_fp32(zo, rows, cin, cout, lead):  # noqa: F811
+    """512 products in a chain, then a rounding for each 512: the bound does not grow with the length.  Equal products,
+    whose roundings in one chain all go the same way, and numbers of either sign."""
+    g = C.rng(47, rows, cin)
+    offsets = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    for x, w in ((torch.full((rows, cin), 0.9), torch.ones(cin, cout)),
+                 (C.normal(g, rows, cin).float(), C.normal(g, cin, cout).float())):
+        want, size = x.double() @ w.double(), x.double().abs() @ w.double().abs()
+        bound = (512 + cin / 512 + 8) * 2 * C.U * size
+        for transposed in (False, True):
+            ww = w.t().contiguous() if transposed else w
+            out = Out(rows, cout, F32, 0, lead)
+            zo.zero_expert_product(put(x, 0, lead), put(ww, 0, lead).unsqueeze(0), offsets, out.view, transposed=transposed)
+            torch.cuda.synchronize()
+            assert out.guards_intact()
+            C.within(out.view, want, C.rounded(bound, want, F32), "y")
