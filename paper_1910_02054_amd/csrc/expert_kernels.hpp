@@ -172,17 +172,18 @@ struct TileShape {
     static_assert(kRowLoads * 16 * kThreads == kRowsBytes && kColLoads * 16 * kThreads == kColsBytes, "whole loads");
 };
 
-// The product's long sums in fp32: what kFoldSteps steps have added up goes into sums of its own, so that no chain of
+// Long sums in fp32: what kFoldSteps steps have added up goes into sums of its own, so that no chain of
 // roundings is longer than 512 products and one for each 512 behind them (in one chain 8193 products of 0.9 were
 // off by 7e-5 of their sum, 262144 by 2e-3).  The 16-bit types add 32 products at a time: up to 131072 of them their roundings of 2^-24 stay
 // below the result's own, 2^-12 or 2^-9.
 constexpr int kFoldSteps = 16;
 
-template <bool USED, typename S>
+template <typename T, typename S>
 struct Folded {
-    f32x4 sum[USED ? S::kTm : 1][USED ? S::kTn : 1];
+    static constexpr bool kUsed = T::kPer == 4;
+    f32x4 sum[kUsed ? S::kTm : 1][kUsed ? S::kTn : 1];
     __device__ __forceinline__ Folded() {
-        if constexpr (USED)
+        if constexpr (kUsed)
 #pragma unroll
             for (int m = 0; m < S::kTm; ++m)
 #pragma unroll
@@ -191,7 +192,7 @@ struct Folded {
     }
     // Behind step s of a tile.
     __device__ __forceinline__ void fold(int s, f32x4 (&acc)[S::kTm][S::kTn]) {
-        if constexpr (USED)
+        if constexpr (kUsed)
             if (s % kFoldSteps == kFoldSteps - 1) {
 #pragma unroll
                 for (int m = 0; m < S::kTm; ++m)
@@ -203,7 +204,7 @@ struct Folded {
             }
     }
     __device__ __forceinline__ void join(f32x4 (&acc)[S::kTm][S::kTn]) const {
-        if constexpr (USED)
+        if constexpr (kUsed)
 #pragma unroll
             for (int m = 0; m < S::kTm; ++m)
 #pragma unroll
@@ -285,8 +286,8 @@ __device__ __forceinline__ void wait_stage() {
 // 1186; the early halves 1146.  Tried and left: steps of 64 bytes in four stages (half lines copied: 1315), lines
 // touched ahead for L2 (1229), four waves of 128 by 128 (2830: one wave a SIMD), stores past the caches, a raised
 // wave priority and groups of 4 or 16 row tiles (no difference).
-template <typename T, typename S, bool DMA, bool FOLD, int EARLY, typename XS, typename WS, typename NEXT, typename COPY,
-          typename PUT, typename STEPS, typename FINISH>
+template <typename T, typename S, bool DMA, int EARLY, typename XS, typename WS, typename NEXT, typename COPY, typename PUT,
+          typename STEPS, typename FINISH>
 __device__ __forceinline__ void multiply_tiles(char* tiles, uint32_t lds, const XS& xs, const WS& ws, NEXT next_step,
                                                COPY copy, PUT put, STEPS tile_steps, FINISH finish) {
     constexpr int kLead = S::kTm / 2, kGroups = 2 * S::kTm;
@@ -331,7 +332,7 @@ __device__ __forceinline__ void multiply_tiles(char* tiles, uint32_t lds, const 
 #pragma unroll
             for (int n = 0; n < S::kTn; ++n)
                 acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-        Folded<FOLD, S> folded;
+        Folded<T, S> folded;
         for (int s = 0; s < steps; ++s) {
             const char* from = tiles + at * S::kStage;
             const uint32_t stage = lds + at * S::kStage;
@@ -724,7 +725,7 @@ __global__ __launch_bounds__(S::kThreads, T::kPer == 4 ? 2 : 1) void k_expert_pr
         for (int n = 0; n < S::kTn; ++n)
             acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    Folded<T::kPer == 4, S> folded;
+    Folded<T, S> folded;
     constexpr int kAhead = kStages - 1;  // stages under way
 #pragma unroll
     for (int s = 0; s < kAhead; ++s)
@@ -940,7 +941,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void k_expert_product_run(c
             look_up(first + i * stride, i);
         wait_stage<0>();
     }
-    multiply_tiles<T, S, DMA, T::kPer == 4, kEarly>(tiles, lds_address(tiles) + wave * 1024, xs, ws, next_step, copy, put,
+    multiply_tiles<T, S, DMA, kEarly>(tiles, lds_address(tiles) + wave * 1024, xs, ws, next_step, copy, put,
                                                     tile_steps, finish);
 }
 
@@ -1082,7 +1083,8 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void k_expert_weight_back(c
     int ring = 0, turn = 0;
     const elem *x = nullptr, *dy = nullptr;
     const int cr = t / kChunks;
-    int xc[kColumns], wc[kColumns];  // columns of this thread's chunks
+    int xc[kColumns], wc[kColumns];  // columns of this thread's chunks; without DMA, in the tile
+    int x_col = 0, dy_col = 0;       // the tile's first ones
     int rows_left = 0;
     uint32_t base = 0;
     uint32_t slot[kLoads];
@@ -1097,12 +1099,17 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void k_expert_weight_back(c
 #pragma unroll
             for (int j = 0; j < kColumns; ++j) {  // rows and columns past the last are not stored
                 const int c = ((t % kChunks) ^ across_exchange<T, kChunks>(cr + j * kRows)) * kPer;
-                xc[j] = (int)m * S::BM + c;
-                wc[j] = (int)n * S::BN + c;
                 if constexpr (DMA) {
-                    xc[j] = xc[j] < a.cols_in ? xc[j] : a.cols_in - kPer;
-                    wc[j] = wc[j] < a.cols_out ? wc[j] : a.cols_out - kPer;
+                    const int xi = (int)m * S::BM + c, wi = (int)n * S::BN + c;
+                    xc[j] = xi < a.cols_in ? xi : a.cols_in - kPer;
+                    wc[j] = wi < a.cols_out ? wi : a.cols_out - kPer;
+                } else {  // the same registers for both
+                    xc[j] = wc[j] = c;
                 }
+            }
+            if constexpr (!DMA) {
+                x_col = (int)m * S::BM;
+                dy_col = (int)n * S::BN;
             }
         }
         x = static_cast<const elem*>(a.x);
@@ -1131,7 +1138,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void k_expert_weight_back(c
         const SlotMap& map = is_x ? a.x_map : a.out_map;
         const uint32_t row = map.mode == 0 ? base + r : (uint32_t)map.row(slot[j]);
         const elem* p = is_x ? x + (int64_t)row * a.ld_x : dy + (int64_t)row * a.ld_w;
-        const int c = is_x ? xc[j % kColumns] : wc[j % kColumns];
+        const int c = is_x ? x_col + xc[j % kColumns] : dy_col + wc[j % kColumns];
         if constexpr (DMA)
             copy_to_lds(there ? p + c : zeros, stage + (is_x ? 0 : S::kRowsBytes) + j * S::kThreads * 16);
         else
@@ -1160,7 +1167,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void k_expert_weight_back(c
         store_sums<T, S>(a, part_place(table, a, id / of_part), acc, (int)m * S::BM + wm * S::kTm * 16,
                          (int)n * S::BN + wn * S::kTn * 16, lane);
     };
-    multiply_tiles<T, S, DMA, false, DMA ? 2 * kHalf : 0>(tiles, lds_address(tiles) + wave * 1024, xs, ws, next_step, copy,
+    multiply_tiles<T, S, DMA, DMA ? 2 * kHalf : 0>(tiles, lds_address(tiles) + wave * 1024, xs, ws, next_step, copy,
                                                           put, tile_steps, finish);
 }
 

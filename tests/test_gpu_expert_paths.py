@@ -206,3 +206,23 @@ def test_long_sums_in_fp32(zo, rows, cin, cout, lead):  # noqa: F811
             torch.cuda.synchronize()
             assert out.guards_intact()
             C.within(out.view, want, C.rounded(bound, want, F32), "y")
+
+
+@pytest.mark.parametrize("lead", (0, 1))
+@pytest.mark.parametrize("rows,cin,cout,parts", ((8193, 2900, 2904, False), (40000, 4100, 4100, False), (100000, 40, 72, True)))
+def test_long_sums_of_the_weights_gradient_in_fp32(zo, rows, cin, cout, parts, lead):  # noqa: F811
+    """As above, over an expert's rows: in one part, or in several whose sums are added up."""
+    n = zo.zero_expert_workspace(rows, 1, cin, cout)
+    assert (n > 0) == parts
+
+    def full(cols, value):
+        return torch.full((lead + rows * cols,), value, device="cuda")[lead:].view(rows, cols)
+
+    out = Out(cin, cout, F32, 0, lead)
+    room = Out(1, n, F32)
+    zo.zero_expert_weight_backward(full(cin, 0.9), full(cout, 1.0), torch.tensor([0, rows], dtype=torch.int32, device="cuda"),
+                                   out.view.unsqueeze(0), room.view[0])
+    torch.cuda.synchronize()
+    assert out.guards_intact() and room.guards_intact()
+    want = rows * torch.tensor(0.9).double().item()
+    assert (out.view.double() - want).abs().max().item() <= (512 + rows / 512 + 8) * 2 * C.U * want
