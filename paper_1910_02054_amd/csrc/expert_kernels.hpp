@@ -1009,7 +1009,9 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void k_expert_weight_back(c
     __shared__ TileTable table;
 
     __shared__ uint32_t costs[ZERO_ROUTE_MAX_EXPERTS];
-    constexpr uint32_t kTileCost = 4;  // of a part's beginning and end, in steps
+    // Of a part's beginning and end, in steps (16384 slots of four of 64 experts, 1024 by 256 bf16: 139 us, 163 with 0 and
+    // 136 with 16; 4096 of 8, 1600 by 6400 f16: 144, 154 and 144).
+    constexpr uint32_t kTileCost = 4;
     fill_tile_table(table, costs, a, [&](int rows) { return parts_of(rows, a.part); },
                     [&](int rows) { return ((uint32_t)rows + kStep - 1) / kStep + kTileCost * parts_of(rows, a.part); });
     const uint32_t m_tiles = ((uint32_t)a.cols_in + S::BM - 1) / S::BM, n_tiles = ((uint32_t)a.cols_out + S::BN - 1) / S::BN;

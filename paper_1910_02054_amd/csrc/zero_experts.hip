@@ -70,7 +70,10 @@ int with_run_shape(int64_t slots, int experts, int64_t cols_out, F f) {
 
 // Rows of a part of the weights' gradient's sums, 0: an expert's rows are one.  A longer part takes longer (1.5 us
 // for 64 rows), a shorter one leaves more sums to be written and read again (at 4.5 TB/s): slots / part matrices
-// of `size` floats. The length at which both are the same, if the workspace's bound allows it.
+// of `size` floats.  The length at which both are the same, 256 at least, if the workspace's bound allows it.  Half and
+// twice that: 65536 slots of 8, 512 by 512 bf16: 68.2 us, 68.7 and 96.3; 16384 of 8, 128 by 256 f16: 23.0, 23.0 and 24.8;
+// 16384 of one of 8, 256 by 256 f16: 44.4, 46.3 and 43.2; 65536 of 64, 512 by 256 bf16: 61.4, 61.4 and 53.2.  128 or 512 at
+// least: 16384 of 16, 128 by 128 fp32: 38.3, 33.5 and 61.1; 16384 of 8, 128 by 256 f16: 23.0, 23.0 and 26.0.
 int64_t part_rows(int64_t slots, int experts, int64_t size) {
     const int64_t room = ZERO_EXPERT_WORKSPACE_MAX / size - experts;  // parts behind each expert's first
     if (room < 1)
@@ -80,7 +83,13 @@ int64_t part_rows(int64_t slots, int experts, int64_t size) {
     return rows < slots ? div_up(rows, 64) * 64 : 0;
 }
 
-constexpr int64_t kFewRows = 48;  // of an expert on average: tiles of 32 rows
+// Slots to an expert on average up to which its rows go in tiles of 32 by 128, a workgroup each, instead of in runs of
+// large tiles: many more workgroups where the experts or columns are few, but every 32 rows copy the weights to LDS
+// again.  Small tiles and large, bf16, 48 rows an expert: 8 experts 4096 to 1024 33.5 us and 67.5, 1024 to 4096 21.3
+// and 24.1; 64 experts 134 and 104, 152 and 119.  8 rows: 31.8 and 66.9, 17.8 and 22.9; 64 experts 99.9 and 98.9, 118 and
+// 109.  128 rows: 50.3 and 69.7, 33.9 and 25.9; 64 experts 211 and 140, 226 and 153.  The host knows the average alone: 2048
+// slots of 64 experts 1024 to 4096 that all chose one take 40.5 us, in large tiles 24.3.
+constexpr int64_t kFewRows = 48;
 constexpr uint32_t kMaxTiles = 1 << 20;  // workgroups of one launch
 
 }  // namespace

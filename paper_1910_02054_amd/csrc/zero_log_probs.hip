@@ -13,17 +13,20 @@ struct LogitShape {
     static constexpr int NT = NT_, NV = NV_;
 };
 
-// Rows of more than 7168 vectors fit a workgroup's registers up to 16384, at one workgroup to a compute unit;
-// where a list follows two that read the row twice are faster (1024 x 131072 bf16 without a list 57.7 us, read
-// again 62; lists of 128: 103 and 85).
+// Threads and vectors a thread, (NT, NV), of a row of so many vectors: the least that hold it, as more leave threads
+// without work.  Full rows at the last size of each, f16, and the next shape's time: 131072 x 1024 80 us and 171, 32768 x
+// 4096 51 and 87, 16384 x 8192 52 and 152, 4096 x 32768 54 and 71, 2340 x 57344 51 and 108.  Longer rows are read as
+// they are needed, two workgroups to a compute unit; 16 vectors a thread leave room for one, which is faster only where
+// there are few rows and long ones (bf16, without a list: 64 x 131072 11.3 us and 12.5, 64 x 100352 10.8 and 10.7, 256 x
+// 131072 18.7 and 16.3, 1024 x 131072 58.3 and 50.8, 1024 x 64000 46.0 and 28.1).
 template <typename F>
-int with_logit_shape(int64_t vectors, bool list, F f) {
+int with_logit_shape(int64_t vectors, int64_t rows, bool list, F f) {
     if (vectors <= 128) return f(LogitShape<128, 1>{});
     if (vectors <= 512) return f(LogitShape<128, 4>{});
     if (vectors <= 1024) return f(LogitShape<256, 4>{});
     if (vectors <= 4 * 1024) return f(LogitShape<512, 8>{});
     if (vectors <= 7 * 1024) return f(LogitShape<1024, 7>{});
-    if (vectors <= 16 * 1024 && !list) return f(LogitShape<1024, 16>{});
+    if (rows <= 64 && vectors > 12 * 1024 && vectors <= 16 * 1024 && !list) return f(LogitShape<1024, 16>{});
     return f(LogitShape<1024, 0>{});
 }
 
@@ -74,7 +77,7 @@ int zero_log_probs(const zero_log_probs_args_t* args, void* stream_) {
     const zo::LogProbScalars k = scalars(a.temperature, 1.0);
     return with_type(a.dtype, [&](auto type) {
         using T = decltype(type);
-        return with_logit_shape(a.vocab / T::kPer, a.k > 0, [&](auto shape) {
+        return with_logit_shape(a.vocab / T::kPer, a.rows, a.k > 0, [&](auto shape) {
             using S = decltype(shape);
             const int capacity = 3 * a.k + 64;  // entries of the list's room, vectors of its queue
             const size_t room = a.k ? (size_t)capacity * 12 : 0;

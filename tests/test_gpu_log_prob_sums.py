@@ -8,6 +8,7 @@ import torch
 
 sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
 import operator_checks as C  # noqa: E402
+from test_gpu_log_probs import check, logits  # noqa: E402
 from test_gpu_operators import zo  # noqa: E402,F401
 
 pytestmark = pytest.mark.gpu
@@ -62,3 +63,10 @@ def test_a_maximum_that_keeps_rising(zo, k):  # noqa: F811
     assert abs(h.item() - (math.log(total) + first)) <= 3 * of_sum + C.U * 30
     if k:
         assert kw["top_index"][0].tolist() == [vocab - 1, vocab - 2, vocab - 3]
+
+
+@pytest.mark.parametrize("dtype", C.TYPES)
+@pytest.mark.parametrize("rows,vocab", ((3, 60000), (64, 131072), (65, 131072), (3, 100000), (3, 28800), (65, 65536)))
+def test_long_rows_without_a_list(zo, rows, vocab, dtype):  # noqa: F811
+    """About the rows and lengths at which the kernel changes, for 8 and for 4 logits a vector."""
+    check(zo, *logits(rows, vocab, dtype, 51), 0)
