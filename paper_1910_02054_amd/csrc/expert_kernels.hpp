@@ -279,13 +279,13 @@ __device__ __forceinline__ void wait_stage() {
 // these, the last EARLY those of the second half. Without DMA a step's copies go to registers a step earlier, and
 // put(stage) writes them to LDS where all waves have met.
 //
-// What bounds it, 16384 x 8 slots 1024 to 4096 bf16 (1140 us, 964 TFLOP/s; batched library products of equal sizes
-// 1086): the products with their fragments' reads alone 733 us, as fast as the library's 8192^3; the copies alone
-// 547; both 985 to 1020, since LDS serves reads and copies by turns and a step's copies have a step's time to
-// land; the stores the rest.  In steps taken: a workgroup a tile 1300; tiles in a run 1245; whole lines stored
-// 1186; the early halves 1146.  Tried and left: steps of 64 bytes in four stages (half lines copied: 1315), lines
-// touched ahead for L2 (1229), four waves of 128 by 128 (2830: one wave a SIMD), stores past the caches, a raised
-// wave priority and groups of 4 or 16 row tiles (no difference).
+// What bounds it, 16384 x 8 slots 1024 to 4096 bf16 (1137 to 1185 us from card to card, 967 to 928 TFLOP/s; batched
+// library products of equal sizes 1086): the products with their fragments' reads alone 733 us, as fast as the library's
+// 8192^3; the copies alone 547; both 985 to 1020, since LDS serves reads and copies by turns and a step's copies have a
+// step's time to land; the stores the rest.  In steps taken, on one card: a workgroup a tile 1300; tiles in a run 1245;
+// whole lines stored 1186; the early halves 1146.  Tried and left: steps of 64 bytes in four stages (half lines copied:
+// 1315), lines touched ahead for L2 (1229), four waves of 128 by 128 (2830: one wave a SIMD), stores past the caches, a
+// raised wave priority and groups of 4 or 16 row tiles (no difference).
 template <typename T, typename S, bool DMA, int EARLY, typename XS, typename WS, typename NEXT, typename COPY, typename PUT,
           typename STEPS, typename FINISH>
 __device__ __forceinline__ void multiply_tiles(char* tiles, uint32_t lds, const XS& xs, const WS& ws, NEXT next_step,
@@ -597,10 +597,14 @@ __device__ __forceinline__ TilePlace tile_place(const TileTable& table, int expe
 }
 
 // ---------------------------------------------------------------------------
-// y = x * weight, a workgroup a tile, for experts of few rows: every weight is read once, and HBM bounds it (48
-// slots of 64 experts 4096 to 1024 bf16: 47 us, 6.2 TB/s).  Four stages of copies are under way.  ALONG: the
-// weights lie [out, in].  DMA: every row of x and of the weights is made of aligned chunks of 16 bytes, which go
-// straight to LDS; else they pass through the registers, where their ends are seen to.
+// y = x * weight, a workgroup a tile, for experts of few rows: every weight is read once, and the loads that a compute
+// unit has under way bound it: three of four stages.  48 slots of 64 experts 4096 to 1024 bf16, one set of weights again
+// and again: 36 to 42 us where they meet up to 32 experts, 256 tiles; 52 to 65 from 33 on, where some compute units have
+// two; sets in turn 51 to 58.  Two slots of 8 experts 14336 to 4096, 64 tiles: 88 us, 2.7 TB/s; one of 4096 to 14336, 112
+// tiles: 21 us, 5.5.
+// ALONG: the weights lie [out, in].  DMA: every row of x and of the weights is made of aligned chunks of 16 bytes, which
+// go straight to LDS; else they pass through the registers, where their ends are seen to, one step ahead (512 slots of 64
+// experts 4096 to 1024 bf16: 100 us, 128 where rows are 2 bytes off a word; 64 of 8, 4095 to 1023 fp32: 368, aligned 87).
 // ---------------------------------------------------------------------------
 // (Two waves a SIMD are asked for in fp32 so that the sums stay in registers that additions take too: kept in the
 // accumulation registers they went back and forth every step, 64 slots of 8 experts 4096 to 1024: 95 us and 87.)
@@ -770,8 +774,8 @@ __global__ __launch_bounds__(S::kThreads, T::kPer == 4 ? 2 : 1) void k_expert_pr
 
 // ---------------------------------------------------------------------------
 // The same in a run of tiles for each workgroup.  Rows of any alignment pass through registers (131072 slots 1024
-// to 4096 bf16: 1795 us where rows are 4 bytes off a line, 2833 where they are 2 off, whose loads the memory
-// pipeline takes apart; read as whole words and shifted 2580 and 2059, left).
+// to 4096 bf16: 1135 us aligned, 1832 where rows are 4 bytes off a line, 2939 where they are 2 off, whose loads the memory
+// pipeline takes apart; read as whole words and shifted 2580 and 2059, where these were 1795 and 2833, left).
 // ---------------------------------------------------------------------------
 template <typename T, typename S, bool ALONG, bool DMA>
 __global__ __launch_bounds__(S::kThreads, S::kWaves) void k_expert_product_run(const ExpertCall a) {
@@ -991,8 +995,8 @@ __device__ __forceinline__ void store_sums(const ExpertCall& a, const PartPlace&
 }
 
 // DMA: rows of x and dy are made of aligned chunks, which go straight to LDS.  Both halves of both operands'
-// copies are early ones.  Bound as the product is (16384 x 8 slots 4096 by 1024 bf16 1230 to 1270 us, 860 to 895
-// TFLOP/s): the products alone 773 us, the copies alone 798; all fragments are read transposed, which takes twice
+// copies are early ones.  Bound as the product is (16384 x 8 slots 4096 by 1024 bf16 1245 to 1297 us from card to card, 883
+// to 848 TFLOP/s): the products alone 773 us, the copies alone 798; all fragments are read transposed, which takes twice
 // the LDS cycles.  Experts' loads differ, so the dies take equal shares of the steps, not of the tiles.
 template <typename T, typename S, bool DMA>
 __global__ __launch_bounds__(S::kThreads, S::kWaves) void k_expert_weight_back(const ExpertCall a) {

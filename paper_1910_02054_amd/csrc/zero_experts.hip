@@ -57,8 +57,8 @@ constexpr int64_t kCus = 256;  // MI355X
 
 // The kernel that takes tiles in a run, in tiles of 256 or 128 rows by 256 columns: the shape whose rounds of
 // tiles over the compute units cost less.  A round of 128 rows is 0.58 of one of 256 (8192 slots of 16 experts
-// 4096 to 1600 f16, 280 tiles in 2 rounds of 256 or 504 in 2 of 128: 205 and 153 us; 4096 of 8 experts 1600 to
-// 6400, 500 in 2 or 900 in 4: 109 and 122).
+// 4096 to 1600 f16, 280 tiles in 2 rounds of 256 or 504 in 2 of 128: 210 and 150 us; 4096 of 8 experts 1600 to
+// 6400, 500 in 2 or 900 in 4: 107 and 124; 131072 of 64, 1024 to 4096 bf16: 1157 and 1338).
 template <typename F>
 int with_run_shape(int64_t slots, int experts, int64_t cols_out, F f) {
     auto rounds = [&](int64_t rows) {
@@ -166,7 +166,7 @@ int zero_expert_product(const zero_expert_product_args_t* args, void* stream_) {
         };
         // fp32: the products take most of the time whatever the tile (a sixteenth of bf16's rate), so small tiles,
         // evenly over the compute units, three workgroups to each (3063 slots of 12 experts 803 to 1203: 102 us, 116
-        // in tiles of 64 by 128, 201 of 128 by 128; 1065 of 8 experts 6943 to 3769: 997 and 1401 of 64 by 128)
+        // in tiles of 64 by 128, 201 of 128 by 128; 1065 of 8 experts 6943 to 3769: 957 and 1401 of 64 by 128)
         if constexpr (T::kPer == 4) {
             using S = zo::TileShape<64, 64, 2, 2, 2>;
             return in_runs(S{}, a.transposed ? (dma ? zo::k_expert_product_run<T, S, true, true>
@@ -243,9 +243,9 @@ int zero_expert_weight_backward(const zero_expert_weight_backward_args_t* args, 
     const bool dma = whole_chunks(a.x, a.ld_x, a.cols_in, e) && whole_chunks(a.dy, a.ld_dy, a.cols_out, e);
     return with_type(a.dtype, [&](auto type) {
         using T = decltype(type);
-        // Tiles of 256 by 256, but where they would be half empty (16384 slots of 64 experts, 128 by 128 f16: 21
-        // us, 27 in tiles of 256; 65536 of 64, 512 by 256 bf16: 80 and 62) and for fp32, bound by the products
-        // (8192 of 8, 1024 by 4096: 835 and 1138).
+        // Tiles of 256 by 256, but where they would be half empty (16384 slots of 64 experts, 128 by 128 f16: 19
+        // us, 24 in tiles of 256; 65536 of 64, 512 by 256 bf16: 80 and 61) and for fp32, bound by the products
+        // (8192 of 8, 1024 by 4096: 720 and 830).
         using Wide = zo::TileShape<256, 256, 2, 4, 2>;
         using Small = zo::TileShape<128, 128, 2, 2, 2>;  // two workgroups to a compute unit
         if (!dma)
