@@ -172,10 +172,10 @@ struct TileShape {
     static_assert(kRowLoads * 16 * kThreads == kRowsBytes && kColLoads * 16 * kThreads == kColsBytes, "whole loads");
 };
 
-// Long sums in fp32: what kFoldSteps steps have added up goes into sums of its own, so that no chain of
-// roundings is longer than 512 products and one for each 512 behind them (in one chain 8193 products of 0.9 were
-// off by 7e-5 of their sum, 262144 by 2e-3).  The 16-bit types add 32 products at a time: up to 131072 of them their roundings of 2^-24 stay
-// below the result's own, 2^-12 or 2^-9.
+// Long sums in fp32: what kFoldSteps steps have added up goes into sums of its own, so that no chain of roundings is
+// longer than 512 products and one for each 512 behind them (in one chain 8193 products of 0.9 were off by 7e-5 of their
+// sum, 262144 by 2e-3).  The 16-bit types add 32 products at a time: up to 131072 of them their roundings of 2^-24
+// stay below the result's own, 2^-12 or 2^-9.
 constexpr int kFoldSteps = 16;
 
 template <typename T, typename S>
@@ -600,7 +600,7 @@ __device__ __forceinline__ TilePlace tile_place(const TileTable& table, int expe
 // y = x * weight, a workgroup a tile, for experts of few rows: every weight is read once, and the loads that a compute
 // unit has under way bound it: three of four stages.  48 slots of 64 experts 4096 to 1024 bf16, one set of weights again
 // and again: 36 to 42 us where they meet up to 32 experts, 256 tiles; 52 to 65 from 33 on, where some compute units have
-// two; sets in turn 51 to 58.  Two slots of 8 experts 14336 to 4096, 64 tiles: 88 us, 2.7 TB/s; one of 4096 to 14336, 112
+// two; sets in turn 49 to 58.  Two slots of 8 experts 14336 to 4096, 64 tiles: 88 us, 2.7 TB/s; one of 4096 to 14336, 112
 // tiles: 21 us, 5.5.
 // ALONG: the weights lie [out, in].  DMA: every row of x and of the weights is made of aligned chunks of 16 bytes, which
 // go straight to LDS; else they pass through the registers, where their ends are seen to, one step ahead (512 slots of 64
